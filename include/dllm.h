@@ -69,6 +69,8 @@ extern "C" {
 #define DLLM_STATUS_BAD_PAGE  2  /* a block-table entry outside [0, n_pages), or a position beyond
                                     max_pages_per_seq * page_tokens (access skipped)              */
 #define DLLM_STATUS_ROWS_CAP  4  /* more masked rows than max_batch * max_q in a refresh call      */
+#define DLLM_STATUS_NOT_FINITE 16 /* dllm_kv4_store met an infinity or a NaN, which 4 bits cannot hold (stored as the group's
+                                    largest value, as 0)                                                   */
 #define DLLM_STATUS_BAD_LENGTH 8 /* a device-resident length disagrees with the host value that sized the
                                     launch: prefix_len[b] outside [0, max_prefix_len], a sequence longer than
                                     max_seqlen, cu_seqlens[0] != 0 or cu_seqlens[B] != total_tokens (the
@@ -390,6 +392,97 @@ int dllm_refresh_cache(dllm_ctx *ctx, void *stream, int B, int total_tokens, int
                        const int32_t *tokens, const int32_t *cu_seqlens, const int32_t *n_commit,
                        const int32_t *block_table, int32_t *cand_token, float *conf,
                        float *entropy);
+
+/* ---- long caches: pages mapped on the device, a cache in 4 bits, attention over parts of the cache ------------------
+ *
+ * dllm_plan_pages makes the block tables of a batch hold exactly the pages its sequences need, without a host read.  Sequence
+ * b needs page entry p iff it holds a position that is still read, in [0, min(keep_head, length[b])) or in [first[b],
+ * length[b]) (rounded out to whole pages).  The free pages are a stack of page ids.  The call does what this order of steps
+ * gives:
+ *   1. every entry >= 0 that is not needed becomes -1 and its page is pushed, sequences in order, entries ascending;
+ *   2. sequence b is granted (granted[b] = 1) iff it misses no entry, or the sum of the missing entries of sequences 0 .. b
+ *      is at most the number of free pages (so nobody overtakes one that waits); others keep what they have (0);
+ *   3. the missing entries of granted sequences pop a page each, sequences in order, entries ascending.
+ * A table starts as -1 everywhere, the stack as the ids 0 .. n_pages-1 in any order.  length[b] = 0 gives everything back.
+ * length[b] outside [0, max_pages_per_seq * page_tokens] or first[b] < 0: the sequence's row is left alone, granted[b] = 0,
+ * DLLM_STATUS_BAD_LENGTH (first[b] > length[b] is read as length[b]).  A released entry outside the pool, a stack that
+ * would overflow (a page given back twice) or a popped id outside the pool: dropped, the entry becomes -1, DLLM_STATUS_BAD_PAGE.
+ * n_free outside [0, pages of the pool] is clamped, DLLM_STATUS_BAD_LENGTH.  Stack entries at n_free and above hold whatever
+ * was pushed or popped there.
+ *   pool DLLM_POOL_KV (the pool of dllm_create) or DLLM_POOL_KV4 (dllm_kv4_attach): whose pages these are
+ *   length dev int32 [B]   first dev int32 [B] or NULL (0)    keep_head >= 0 (host)
+ *   block_table dev int32 [B, max_pages_per_seq] in/out   free_pages dev int32 [pages of the pool] in/out
+ *   n_free dev int32 [1] in/out   granted dev int32 [B] or NULL
+ *
+ * dllm_slot_map lists where positions live: for the positions [start[b], end[b]) of the sequences, packed in order, slot =
+ * page * page_tokens + position % page_tokens, or -1 where the table maps no page of the pool.  cu[b] = positions of the sequences
+ * before b, cu[B] all of them.  slots has room for `capacity` entries (host value); those behind the last position become -1,
+ * positions that do not fit are left out (DLLM_STATUS_BAD_LENGTH), as are positions outside the table (ditto).  end[b] < start[b]
+ * lists nothing.
+ *   start, end dev int32 [B]   cu dev int32 [B + 1]   slots dev int32 [capacity] */
+#define DLLM_POOL_KV  0
+#define DLLM_POOL_KV4 1
+int dllm_plan_pages(dllm_ctx *ctx, void *stream, int pool, int B, int keep_head, const int32_t *length, const int32_t *first,
+                    int32_t *block_table, int32_t *free_pages, int32_t *n_free, int32_t *granted);
+int dllm_slot_map(dllm_ctx *ctx, void *stream, int pool, int B, int capacity, const int32_t *start, const int32_t *end,
+                  const int32_t *block_table, int32_t *cu, int32_t *slots);
+
+/* A cache in 4 bits beside the pool of dllm_create, for positions that no longer change (DLLM_BF16 models whose page_tokens is
+ * a multiple of 32; pages of it are page_tokens long too and have block tables of their own, max_pages_per_seq entries a row).  A
+ * value is one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign (codes 0 .. 7, sign in bit 3) times a power of two 2^(byte - 127) that 32
+ * values share: 32 channels of one key, and 32 consecutive positions of one channel of V (the order in which the scaled matrix
+ * instructions sum, so that attention reads both as they lie).  The power of two is the smallest s in 2^-120 .. 2^125 with max|x| <= 7 s
+ * (2^125 for what is beyond); x / s is rounded to the nearest value, half-way to the even code (what lies above 6 becomes 6).
+ * Per layer, page p, kv head h and group g of 32 slots there is one record of 34 * head_dim bytes, at
+ * ((layer * n_pages4 + p) * n_kv_heads + h) * (page_tokens / 32) + g:
+ *   K codes  [32 slots][head_dim / 2]     V codes [head_dim][16]     (even index in the low half of a byte)
+ *   K scales [slot / 16][slot % 4][channel / 32][slot / 4 % 4]     V scales [channel % 16][channel / 16]
+ * dllm_kv4_attach borrows pool4 (dev, 256-byte aligned, dllm_kv4_pool_bytes) for the life of the context or until the next
+ * call (pool4 NULL: detached).  It enqueues nothing.  dllm_kv4_pool_bytes is 0 for configurations without such a cache. */
+size_t dllm_kv4_pool_bytes(const dllm_config *cfg, int n_pages4);
+int dllm_kv4_attach(dllm_ctx *ctx, void *pool4, size_t pool4_bytes, int n_pages4);
+
+/* dllm_kv4_store puts cached positions away: the K and V states of every layer at slot src_slots[i] of the pool of dllm_create
+ * go to slot dst_slots[i] of the 4-bit pool.  Entries come in groups of 32 that share scales: the 32 dst_slots of a group are the
+ * consecutive slots of one record (the first a multiple of 32), its 32 src_slots are any.  A group of which any other entry is -1
+ * or wrong is left out (DLLM_STATUS_BAD_PAGE, but for a group whose dst_slots are all -1, as dllm_slot_map fills up with).
+ * A value that is not finite sets DLLM_STATUS_NOT_FINITE and is stored as the largest value of its 32 with its sign (infinity) or
+ * as 0 (NaN); the scale is that of the finite ones.
+ * dllm_kv4_load brings positions back: slot src_slots[i] of the 4-bit pool to slot dst_slots[i] of the other, value by value (no rounding:
+ * bfloat16 holds them), any slots, -1 in both: left out, in one or out of range: left out, DLLM_STATUS_BAD_PAGE.
+ * No slot may be written twice by one call.
+ *   n_tokens >= 1, for the store a multiple of 32; src_slots, dst_slots dev int32 [n_tokens], as dllm_slot_map writes them */
+int dllm_kv4_store(dllm_ctx *ctx, void *stream, int n_tokens, const int32_t *src_slots, const int32_t *dst_slots);
+int dllm_kv4_load(dllm_ctx *ctx, void *stream, int n_tokens, const int32_t *src_slots, const int32_t *dst_slots);
+
+/* What the rows of a step read of the cache.
+ *   window 0: every key.  window > 0: the row at position p reads key j iff j < n_sink or j > p - window (the rows in flight behind p
+ *   are keys of every row, as in dllm_denoise_step), so a row's own key is the last of `window` at least.
+ *   len4 NULL: every key lies in the pool of dllm_create.  Otherwise keys [0, len4[b]) lie in the 4-bit pool, where table4 maps
+ *   them, and only the others in the pool of dllm_create.  len4[b] is a multiple of 32 in [0, prefix_len[b]] (else rounded down
+ *   into that range, DLLM_STATUS_BAD_LENGTH).
+ * Entries of the block tables that map no key that is read are not looked at.  A key whose entry is outside the pool is left
+ * out (DLLM_STATUS_BAD_PAGE).  What a row does not read does not reach it, whatever it holds. */
+typedef struct {
+  int32_t window, n_sink;           /* >= 0                                                          */
+  const int32_t *len4, *table4;     /* dev int32 [B], [B, max_pages_per_seq]; both or neither        */
+} dllm_cache_view;
+
+/* The attention of one layer alone: softmax(q k / sqrt(head_dim)) v of the rows j < q_valid[b] (all Q if NULL; clamped to [0,
+ * Q], a negative entry leaves the sequence out) of sequence b at positions prefix_len[b] + j over the cached keys [0, prefix_len[b]
+ * + q_valid[b]) that `view` (NULL: all of them, none in 4 bits) lets them read.  Query head h reads kv head h / (n_q_heads /
+ * n_kv_heads).  Other rows of out are left as they are.  Sums and statistics are float; out is rounded once.  A row without a finite
+ * score is NaN.
+ *   q, out dev [B, Q, n_q_heads, head_dim] of the model's type, 16-byte aligned, distinct   other arguments as for dllm_denoise_step_var */
+int dllm_attend(dllm_ctx *ctx, void *stream, int layer, int B, int Q, int max_prefix_len, const void *q, const int32_t *prefix_len,
+                const int32_t *q_valid, const int32_t *block_table, const dllm_cache_view *view, void *out);
+
+/* dllm_denoise_step_var (q_valid NULL: every row valid) whose rows read what `view` says: the step of a long sequence whose complete
+ * positions lie in 4 bits, or of which only the first positions and a window are read.  The rows' K and V go to the pool of
+ * dllm_create as ever.  Prefill and refresh read everything of their forward. */
+int dllm_denoise_step_view(dllm_ctx *ctx, void *stream, int B, int Q, int max_prefix_len, const int32_t *q_tokens,
+                           const int32_t *prefix_len, const int32_t *q_valid, const int32_t *block_table,
+                           const dllm_cache_view *view, int32_t *cand_token, float *conf, float *entropy);
 
 /* Test hooks.  dllm_debug_logits runs the same forward as dllm_denoise_step and stores the raw
  * logits (mask_id column included) of all B*Q rows as float [B, Q, vocab].  dllm_debug_hidden

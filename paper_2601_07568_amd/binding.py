@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(HERE, "libdllm.so")
 
 DLLM_OK, DLLM_EINVAL, DLLM_ESHAPE, DLLM_ENOSPACE, DLLM_EHIP = 0, -1, -2, -3, -4
 DLLM_F32, DLLM_BF16 = 0, 1
-STATUS_BAD_TOKEN, STATUS_BAD_PAGE, STATUS_ROWS_CAP, STATUS_BAD_LENGTH = 1, 2, 4, 8
+STATUS_BAD_TOKEN, STATUS_BAD_PAGE, STATUS_ROWS_CAP, STATUS_BAD_LENGTH, STATUS_NOT_FINITE = 1, 2, 4, 8, 16
+POOL_KV, POOL_KV4 = 0, 1
 
 
 class Config(C.Structure):
@@ -35,6 +36,10 @@ class LayerW(C.Structure):
 class Weights(C.Structure):
     _fields_ = [("tok_emb", C.c_void_p), ("final_norm", C.c_void_p), ("lm_head", C.c_void_p),
                 ("layers", C.POINTER(LayerW))]
+
+
+class CacheView(C.Structure):
+    _fields_ = [("window", C.c_int32), ("n_sink", C.c_int32), ("len4", C.c_void_p), ("table4", C.c_void_p)]
 
 
 _lib = None
@@ -90,6 +95,14 @@ def lib() -> C.CDLL:
                                     C.POINTER(C.c_double)]),
         "dllm_probe_hbm_read": (i32, [vp, vp, vp, sz, vp]),
         "dllm_probe_mfma": (i32, [vp, vp, i32, i32, vp, C.POINTER(C.c_double)]),
+        "dllm_plan_pages": (i32, [vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]),
+        "dllm_slot_map": (i32, [vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]),
+        "dllm_kv4_pool_bytes": (sz, [pcfg, i32]),
+        "dllm_kv4_attach": (i32, [vp, vp, sz, i32]),
+        "dllm_kv4_store": (i32, [vp, vp, i32, vp, vp]),
+        "dllm_kv4_load": (i32, [vp, vp, i32, vp, vp]),
+        "dllm_attend": (i32, [vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, C.POINTER(CacheView), vp]),
+        "dllm_denoise_step_view": (i32, [vp, vp, i32, i32, i32, vp, vp, vp, vp, C.POINTER(CacheView), vp, vp, vp]),
         "dllm_strerror": (C.c_char_p, [i32]),
         "dllm_last_hip_error": (C.c_char_p, [vp]),
     }
@@ -342,6 +355,84 @@ class Engine:
         self._check(lib().dllm_refresh_cache(self.ctx, self._stream(), B, total_tokens, max_seqlen, _ptr(tokens),
                                              _ptr(cu_seqlens), _ptr(n_commit), _ptr(block_table), _ptr(cand),
                                              _ptr(conf), _ptr(entropy)))
+
+    # -- long caches
+    def _dev(self, name, t, dtype, *shape, optional=False):
+        """Pointer of a contiguous tensor of this device; the calls below check what the library cannot see."""
+        if t is None and optional:
+            return None
+        if t.device != self.kv_pool.device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {list(shape)} on {self.kv_pool.device}, got {t.dtype} "
+                             f"{list(t.shape)} with strides {list(t.stride())} on {t.device}")
+        return C.c_void_p(t.data_ptr())
+
+    def _call(self, fn, *args):
+        """One library call on the current stream of the engine's device, with that device current."""
+        with self.torch.cuda.device(self.device):
+            self._check(fn(self.ctx, self._stream(), *args))
+
+    def attach_kv4(self, n_pages4: int):
+        """A pool of n_pages4 pages in 4 bits beside the engine's (0: takes it away again)."""
+        self.kv4_pool = None
+        if n_pages4 == 0:
+            self._check(lib().dllm_kv4_attach(self.ctx, None, 0, 0))
+            return
+        n = lib().dllm_kv4_pool_bytes(C.byref(self.cfg), n_pages4)
+        if n == 0 and self.ms.n_layers > 0:
+            raise DllmError(DLLM_ESHAPE, "(no 4-bit cache of this model, page size or number of pages)")
+        pool = self.torch.zeros(max(n, 1), dtype=self.torch.uint8, device=self.device)   # (the allocator aligns to 512 bytes)
+        self._check(lib().dllm_kv4_attach(self.ctx, C.c_void_p(pool.data_ptr()), n, n_pages4))
+        self.kv4_pool, self.n_pages4 = pool, n_pages4
+
+    def _pool(self, kv4):
+        if kv4 and getattr(self, "kv4_pool", None) is None:
+            raise DllmError(DLLM_EINVAL, "(no 4-bit pool attached)")
+        return (POOL_KV4, self.n_pages4) if kv4 else (POOL_KV, self.cfg.n_pages)
+
+    def plan_pages(self, length, block_table, free_pages, n_free, granted=None, *, first=None, keep_head=0, kv4=False):
+        i32, (pool, n_pages), B = self.torch.int32, self._pool(kv4), length.numel()
+        self._call(lib().dllm_plan_pages, pool, B, keep_head, self._dev("length", length, i32, B),
+                   self._dev("first", first, i32, B, optional=True),
+                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq),
+                   self._dev("free_pages", free_pages, i32, n_pages), self._dev("n_free", n_free, i32, 1),
+                   self._dev("granted", granted, i32, B, optional=True))
+
+    def slot_map(self, start, end, block_table, cu, slots, *, kv4=False):
+        i32, (pool, _), B = self.torch.int32, self._pool(kv4), start.numel()
+        self._call(lib().dllm_slot_map, pool, B, slots.numel(), self._dev("start", start, i32, B), self._dev("end", end, i32, B),
+                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq), self._dev("cu", cu, i32, B + 1),
+                   self._dev("slots", slots, i32, slots.numel()))
+
+    def kv4_store(self, src_slots, dst_slots):
+        i32, n = self.torch.int32, src_slots.numel()
+        self._call(lib().dllm_kv4_store, n, self._dev("src_slots", src_slots, i32, n), self._dev("dst_slots", dst_slots, i32, n))
+
+    def kv4_load(self, src_slots, dst_slots):
+        i32, n = self.torch.int32, src_slots.numel()
+        self._call(lib().dllm_kv4_load, n, self._dev("src_slots", src_slots, i32, n), self._dev("dst_slots", dst_slots, i32, n))
+
+    def _view(self, B, window, n_sink, len4, table4):
+        i32 = self.torch.int32
+        return C.byref(CacheView(window, n_sink, self._dev("len4", len4, i32, B, optional=True),
+                                 self._dev("table4", table4, i32, B, self.cfg.max_pages_per_seq, optional=True)))
+
+    def attend(self, layer, q, prefix_len, block_table, out, *, max_prefix_len, q_valid=None, window=0, n_sink=0, len4=None,
+               table4=None):
+        i32, (B, Q) = self.torch.int32, q.shape[:2]
+        shape = (B, Q, self.cfg.n_q_heads, self.cfg.head_dim)
+        self._call(lib().dllm_attend, layer, B, Q, max_prefix_len, self._dev("q", q, self.tdtype, *shape),
+                   self._dev("prefix_len", prefix_len, i32, B), self._dev("q_valid", q_valid, i32, B, optional=True),
+                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq),
+                   self._view(B, window, n_sink, len4, table4), self._dev("out", out, self.tdtype, *shape))
+
+    def denoise_step_view(self, q_tokens, prefix_len, block_table, cand, conf, entropy=None, *, max_prefix_len, q_valid=None,
+                          window=0, n_sink=0, len4=None, table4=None):
+        i32, f32, (B, Q) = self.torch.int32, self.torch.float32, q_tokens.shape
+        self._call(lib().dllm_denoise_step_view, B, Q, max_prefix_len, self._dev("q_tokens", q_tokens, i32, B, Q),
+                   self._dev("prefix_len", prefix_len, i32, B), self._dev("q_valid", q_valid, i32, B, optional=True),
+                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq),
+                   self._view(B, window, n_sink, len4, table4), self._dev("cand", cand, i32, B, Q),
+                   self._dev("conf", conf, f32, B, Q), self._dev("entropy", entropy, f32, B, Q, optional=True))
 
     def debug_logits(self, q_tokens, prefix_len, block_table, *, max_prefix_len):
         B, Q = q_tokens.shape

@@ -64,6 +64,7 @@ static bool build_map(const dllm_config* c, Workspace* m) {
   m->tok_seq = take(t_max * 4);
   m->tok_pos = take(t_max * 4);
   m->kv_loc = m->q32;   // a forward uses one or the other (16 bytes a token of at least 256), so no call needs more workspace for it
+  m->plan = m->q32;     // (16 bytes and 8 a sequence; nothing of a forward outlives it)
   m->rows = take((size_t)m->r_max * 4);
   m->lm_part = take((size_t)m->r_max * ((c->vocab + 63) / 64) * 4 * 4);   // finest split: 64 columns per partial
   m->attn_rows = (int64_t)t_step * c->n_q_heads * 8;
@@ -448,7 +449,8 @@ static int run_forward_inner(dllm_ctx* c, hipStream_t s, const StepGeom& g, int 
     }
     {
       ProfScope p(c, s, 5, 2.0 * 2.0 * dkv * (double)g.max_kv * g.B);
-      if (s32) TRY(launch_s32_attn(c, s, g, attention_view(c, g, l)), "attention");
+      if (g.view) TRY(launch_attend(c, s, g, l, c->ws + c->map.q, c->ws + c->map.o, sk ? (T + 15) / 16 : 0), "attention");
+      else if (s32) TRY(launch_s32_attn(c, s, g, attention_view(c, g, l)), "attention");
       else if (attn_step_supported(c, g)) TRY(launch_attn_step(c, s, g, attention_view(c, g, l), sk), "attention");
       else TRY(launch_attention_generic(c, s, g, l), "attention");
     }
@@ -750,6 +752,111 @@ extern "C" int dllm_refresh_cache_dev(dllm_ctx* c, void* stream, int B, int toke
   if (!conf) return DLLM_EINVAL;
   HeadOut h{cand_token, conf, entropy};
   return packed_forward(c, stream, B, token_capacity, max_seqlen, tokens, cu_seqlens, n_commit, block_table, &h, true);
+}
+
+// ---- long caches -----------------------------------------------------------------------------------
+static bool kv4_config_ok(const dllm_config* c) { return config_ok(c) && c->dtype == DLLM_BF16 && c->page_tokens % 32 == 0; }
+// slots of a pool are numbered in 31 bits
+static bool slots_fit(const dllm_config& f, int n_pages) { return (int64_t)n_pages * f.page_tokens < ((int64_t)1 << 31); }
+
+extern "C" size_t dllm_kv4_pool_bytes(const dllm_config* cfg, int n_pages4) {
+  if (!kv4_config_ok(cfg) || n_pages4 < 1 || !slots_fit(*cfg, n_pages4)) return 0;
+  return (size_t)cfg->n_layers * n_pages4 * cfg->n_kv_heads * (cfg->page_tokens / 32) * 34 * cfg->head_dim;
+}
+
+extern "C" int dllm_kv4_attach(dllm_ctx* c, void* pool4, size_t pool4_bytes, int n_pages4) {
+  if (!c) return DLLM_EINVAL;
+  if (!pool4) { c->kv4_pool = nullptr; c->n_pages4 = 0; return DLLM_OK; }
+  if (n_pages4 < 1 || ((uintptr_t)pool4 & 255) != 0) return DLLM_EINVAL;
+  if (!kv4_config_ok(&c->cfg) || !slots_fit(c->cfg, n_pages4)) return DLLM_ESHAPE;
+  if (pool4_bytes < dllm_kv4_pool_bytes(&c->cfg, n_pages4)) return DLLM_ENOSPACE;
+  c->kv4_pool = (uint8_t*)pool4;
+  c->n_pages4 = n_pages4;
+  return DLLM_OK;
+}
+
+// pages of a pool; 0: there is no such pool
+static int pool_pages(const dllm_ctx* c, int pool) {
+  return pool == DLLM_POOL_KV ? c->cfg.n_pages : (pool == DLLM_POOL_KV4 && c->kv4_pool ? c->n_pages4 : 0);
+}
+
+extern "C" int dllm_plan_pages(dllm_ctx* c, void* stream, int pool, int B, int keep_head, const int32_t* length, const int32_t* first,
+                               int32_t* block_table, int32_t* free_pages, int32_t* n_free, int32_t* granted) {
+  if (!c || !length || !block_table || !free_pages || !n_free) return DLLM_EINVAL;
+  if (B < 1 || keep_head < 0 || pool_pages(c, pool) == 0) return DLLM_EINVAL;
+  if (B > c->cfg.max_batch) return DLLM_ESHAPE;
+  TRY(launch_plan_pages(c, (hipStream_t)stream, pool_pages(c, pool), B, keep_head, length, first, block_table, free_pages, n_free, granted),
+      "plan_pages");
+  return DLLM_OK;
+}
+
+extern "C" int dllm_slot_map(dllm_ctx* c, void* stream, int pool, int B, int capacity, const int32_t* start, const int32_t* end,
+                             const int32_t* block_table, int32_t* cu, int32_t* slots) {
+  if (!c || !start || !end || !block_table || !cu || !slots) return DLLM_EINVAL;
+  if (B < 1 || capacity < 1 || pool_pages(c, pool) == 0) return DLLM_EINVAL;
+  const int64_t row = (int64_t)c->cfg.max_pages_per_seq * c->cfg.page_tokens;
+  if (B > c->cfg.max_batch || row >= ((int64_t)1 << 31) / B || !slots_fit(c->cfg, pool_pages(c, pool))) return DLLM_ESHAPE;
+  TRY(launch_slot_map(c, (hipStream_t)stream, pool_pages(c, pool), B, capacity, start, end, block_table, cu, slots), "slot_map");
+  return DLLM_OK;
+}
+
+static int check_kv4_move(dllm_ctx* c, int n_tokens, const void* src, const void* dst) {
+  if (!c || !src || !dst || n_tokens < 1 || !c->kv4_pool) return DLLM_EINVAL;
+  if (!slots_fit(c->cfg, c->cfg.n_pages) || c->cfg.n_kv_heads > 65535 || c->cfg.n_layers > 65535) return DLLM_ESHAPE;
+  return DLLM_OK;
+}
+
+extern "C" int dllm_kv4_store(dllm_ctx* c, void* stream, int n_tokens, const int32_t* src_slots, const int32_t* dst_slots) {
+  const int rc = check_kv4_move(c, n_tokens, src_slots, dst_slots);
+  if (rc != DLLM_OK) return rc;
+  if (n_tokens % 32 != 0) return DLLM_EINVAL;
+  TRY(launch_kv4_store(c, (hipStream_t)stream, n_tokens, src_slots, dst_slots), "kv4_store");
+  return DLLM_OK;
+}
+
+extern "C" int dllm_kv4_load(dllm_ctx* c, void* stream, int n_tokens, const int32_t* src_slots, const int32_t* dst_slots) {
+  const int rc = check_kv4_move(c, n_tokens, src_slots, dst_slots);
+  if (rc != DLLM_OK) return rc;
+  TRY(launch_kv4_load(c, (hipStream_t)stream, n_tokens, src_slots, dst_slots), "kv4_load");
+  return DLLM_OK;
+}
+
+static int check_view(const dllm_ctx* c, const dllm_cache_view* v) {
+  if (!v) return DLLM_OK;
+  if (v->window < 0 || v->n_sink < 0 || (v->len4 == nullptr) != (v->table4 == nullptr)) return DLLM_EINVAL;
+  if (v->len4 && !c->kv4_pool) return DLLM_EINVAL;
+  return DLLM_OK;
+}
+
+extern "C" int dllm_attend(dllm_ctx* c, void* stream, int layer, int B, int Q, int max_prefix_len, const void* q,
+                           const int32_t* prefix_len, const int32_t* q_valid, const int32_t* block_table,
+                           const dllm_cache_view* view, void* out) {
+  int rc = check_step_args(c, B, Q, max_prefix_len, q, prefix_len, block_table, q_valid != nullptr);
+  if (rc != DLLM_OK) return rc;
+  if (!out || q == out || layer < 0 || layer >= c->cfg.n_layers || (((uintptr_t)q | (uintptr_t)out) & 15) != 0) return DLLM_EINVAL;
+  rc = check_view(c, view);
+  if (rc != DLLM_OK) return rc;
+  const dllm_cache_view all = {0, 0, nullptr, nullptr};
+  StepGeom g = step_geom(B, Q, max_prefix_len, nullptr, prefix_len, block_table);
+  g.q_valid = q_valid;
+  g.view = view ? view : &all;
+  TRY(launch_attend(c, (hipStream_t)stream, g, layer, q, out, 0), "attend");
+  return DLLM_OK;
+}
+
+extern "C" int dllm_denoise_step_view(dllm_ctx* c, void* stream, int B, int Q, int max_prefix_len, const int32_t* q_tokens,
+                                      const int32_t* prefix_len, const int32_t* q_valid, const int32_t* block_table,
+                                      const dllm_cache_view* view, int32_t* cand_token, float* conf, float* entropy) {
+  int rc = check_step_args(c, B, Q, max_prefix_len, q_tokens, prefix_len, block_table, q_valid != nullptr);
+  if (rc != DLLM_OK) return rc;
+  if (!cand_token || !conf) return DLLM_EINVAL;
+  rc = check_view(c, view);
+  if (rc != DLLM_OK) return rc;
+  StepGeom g = step_geom(B, Q, max_prefix_len, q_tokens, prefix_len, block_table);
+  g.q_valid = q_valid;
+  if (view && (view->window > 0 || view->len4)) g.view = view;   // (else: the step that reads everything)
+  HeadOut h{cand_token, conf, entropy};
+  return run_forward(c, (hipStream_t)stream, g, c->cfg.n_layers, &h, nullptr, nullptr);
 }
 
 extern "C" int dllm_unmask(dllm_ctx* c, void* stream, int B, int Q, int block_len, int32_t* q_tokens,

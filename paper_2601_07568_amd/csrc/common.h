@@ -224,6 +224,7 @@ struct Workspace {
   size_t qkvp;         // float [LG_QKV_SPLITS][lg_delta_rows, dq + 2 dkv]: K-split partial sums of the fused q/k/v product
   int64_t qkvp_stride;
   int64_t qkvp_rows;   // rows a single (unsplit) product may have
+  size_t plan;         // int32 [4 + 2 * max_batch]     page planning: sums of what the sequences give back and miss; in q32's place
   size_t scratch;      // general scratch for fast kernels (split-K partials)
   size_t total;
   int64_t t_max, r_max, t_step, tpad;
@@ -242,6 +243,8 @@ struct dllm_ctx {
   dllm_layer_w* packed_layers;   // host array; norm gains are not packed and left null
   const void* packed_lm_head;
   char* kv_pool;
+  uint8_t* kv4_pool;         // dllm_kv4_attach (nullptr: none)
+  int n_pages4;
   char* ws;
   dllm::Workspace map;
   int kernel_mode;
@@ -280,6 +283,7 @@ struct StepGeom {           // which tokens a forward runs over
   bool total_is_cap = false;   // packed: T is the capacity of the token buffer, the device-resident total may be smaller
   const int32_t* n_cache;      // dev [B] or nullptr (packed: how many positions go to the pool)
   const int32_t* block_table;  // dev [B, max_pages]
+  const dllm_cache_view* view = nullptr;   // step: which keys its rows read (host record), or nullptr: all of them, none in 4 bits
 };
 
 // kv_loc: also leave every row's K/V destination in the workspace (and report pages that are not addressable)
@@ -351,6 +355,16 @@ hipError_t launch_fsm_plan(hipStream_t s, int B, int n_blocks, int block_len, co
 hipError_t launch_copy_f32(hipStream_t s, const float* src, float* dst, size_t n);
 hipError_t launch_gather_rows(hipStream_t s, int B, int row_len, const int32_t* index, const int32_t* n_index,
                               const int32_t* src, int32_t* dst, int32_t fill, bool scatter);
+
+// ---- launchers implemented in kernels_cache.hip / kernels_attend.hip ------------------------------------------------
+hipError_t launch_plan_pages(dllm_ctx* c, hipStream_t s, int n_pages, int B, int keep_head, const int32_t* length, const int32_t* first,
+                             int32_t* table, int32_t* stack, int32_t* n_free, int32_t* granted);
+hipError_t launch_slot_map(dllm_ctx* c, hipStream_t s, int n_pages, int B, int capacity, const int32_t* start, const int32_t* end,
+                           const int32_t* table, int32_t* cu, int32_t* slots);
+hipError_t launch_kv4_store(dllm_ctx* c, hipStream_t s, int n_tokens, const int32_t* src, const int32_t* dst);
+hipError_t launch_kv4_load(dllm_ctx* c, hipStream_t s, int n_tokens, const int32_t* src, const int32_t* dst);
+// attention of a step over what g.view lets its rows read: q and o of the model's type, o row-major or, out_mt > 0, in fragment order
+hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int layer, const void* q, void* o, int out_mt);
 
 // ---- launchers implemented in kernels_skinny.hip / _attention.hip / _gemm.hip (bf16, matrix cores) ------
 bool mfma_supported(const dllm_ctx* c);

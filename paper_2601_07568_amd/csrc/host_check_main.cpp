@@ -222,6 +222,20 @@ int main(int argc, char** argv) {
     EXPECT(dllm_eos_scan(ctx, nullptr, 1, 32, ip, 5, ip, nullptr, ip, nullptr), DLLM_EINVAL);
     EXPECT(dllm_gather_rows(ctx, nullptr, 2, 4, ip, ip, ip, ip, 0), DLLM_EINVAL);
     EXPECT(dllm_scatter_rows(ctx, nullptr, 0, 4, ip, ip, ip, ip + 64), DLLM_EINVAL);
+    // long caches
+    EXPECT(dllm_plan_pages(ctx, nullptr, DLLM_POOL_KV, 3, 0, ip, nullptr, ip, ip, ip, nullptr), DLLM_ESHAPE);
+    EXPECT(dllm_plan_pages(ctx, nullptr, DLLM_POOL_KV4, 1, 0, ip, nullptr, ip, ip, ip, nullptr), DLLM_EINVAL);
+    EXPECT(dllm_slot_map(ctx, nullptr, DLLM_POOL_KV, 1, 0, ip, ip, ip, ip, ip), DLLM_EINVAL);
+    EXPECT(dllm_kv4_store(ctx, nullptr, 32, ip, ip), DLLM_EINVAL);
+    EXPECT(dllm_kv4_load(ctx, nullptr, 32, ip, ip), DLLM_EINVAL);
+    EXPECT(dllm_kv4_attach(ctx, wsp, 1 << 20, 1), DLLM_ESHAPE);     // (pages of 16)
+    EXPECT(dllm_kv4_pool_bytes(&cfg, 4), 0);
+    const dllm_cache_view bad_view = {-1, 0, nullptr, nullptr}, no_pool = {0, 0, ip, ip};
+    EXPECT(dllm_attend(ctx, nullptr, 2, 1, 32, 64, p, ip, nullptr, ip, nullptr, wsp), DLLM_EINVAL);
+    EXPECT(dllm_attend(ctx, nullptr, 0, 1, 32, 64, p, ip, nullptr, ip, &bad_view, wsp), DLLM_EINVAL);
+    EXPECT(dllm_attend(ctx, nullptr, 0, 1, 32, 64, p, ip, nullptr, ip, &no_pool, wsp), DLLM_EINVAL);
+    EXPECT(dllm_denoise_step_view(ctx, nullptr, 1, 32, 64, ip, ip, nullptr, ip, &bad_view, ip, fp, nullptr), DLLM_EINVAL);
+    EXPECT(dllm_denoise_step_view(ctx, nullptr, 1, 33, 64, ip, ip, nullptr, ip, nullptr, ip, fp, nullptr), DLLM_ESHAPE);
     EXPECT(dllm_set_kernel_mode(ctx, 7), DLLM_EINVAL);
     EXPECT(dllm_set_kernel_mode(ctx, 1), DLLM_OK);
     EXPECT(dllm_read_status(ctx, nullptr, nullptr), DLLM_EINVAL);

@@ -1,0 +1,624 @@
+"""Long caches on the GPU: pages planned on the device, the 4-bit pool, attention over parts of the cache, against the float64
+definitions of tests/long_cache.py."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import dllm_oracle as O
+from paper_2601_07568_amd import binding as B
+from paper_2601_07568_amd import synth
+from tests import harness as H
+from tests import long_cache as R
+
+pytestmark = pytest.mark.gpu
+
+SMALL = synth.ModelShape(1, 64, 6, 3, 64, 64, 64, 63)                       # 2 query heads a key head
+HEADS = {"6/3x64": (6, 3, 64), "4/4x64": (4, 4, 64), "8/2x128": (8, 2, 128), "28/4x128": (28, 4, 128), "5/5x128": (5, 5, 128)}
+
+
+def engine(heads="6/3x64", dtype="bf16", layers=1, **kw):
+    hq, hkv, dh = HEADS[heads]
+    ms = dataclasses.replace(SMALL, n_layers=layers, n_q_heads=hq, n_kv_heads=hkv, head_dim=dh, dtype=dtype)
+    return H.make_engine(ms, synth.Weights(ms, 0), pack=False, **kw)
+
+
+# ------------------------------------------------------------------------------------------------ pages and slots
+
+@pytest.mark.parametrize("Bn,NP,pt,n_pages", [(1, 1, 1, 1), (1, 300, 16, 200), (3, 5, 4, 9), (8, 40, 64, 170), (70, 33, 32, 1500), (1500, 7, 16, 6000)])
+@pytest.mark.parametrize("partial", [False, True])
+def test_plan_pages_rounds(Bn, NP, pt, n_pages, partial):
+    """Rounds of growing, ending and (partial) giving back what lies between a head and a tail, with a stack that runs short."""
+    rng = np.random.default_rng(Bn * 1000 + NP)
+    eng = engine(page_tokens=pt, max_pages_per_seq=NP, n_pages=n_pages, max_batch=Bn, max_q=1)
+    table, stack, n_free = [[-1] * NP for _ in range(Bn)], rng.permutation(n_pages).tolist(), n_pages
+    d_table, d_stack, d_free = eng.i32(table), eng.i32(stack), eng.i32([n_free])
+    granted = eng.i32([7] * Bn)
+    length = np.zeros(Bn, dtype=np.int64)
+    for rnd in range(6):
+        length = np.where(rng.random(Bn) < 0.2, 0, np.minimum(NP * pt, length + rng.integers(0, NP * pt // 2 + 2, Bn)))
+        first = np.maximum(0, length - rng.integers(0, NP * pt // 2 + 1, Bn)) if partial else None
+        keep = int(rng.integers(0, 3 * pt)) if partial else 0
+        eng.plan_pages(eng.i32(length), d_table, d_stack, d_free, granted if rnd else None, first=None if first is None else eng.i32(first),
+                       keep_head=keep)
+        table, stack, n_free, g, bad_len, bad_page = R.plan_pages(pt, n_pages, keep, length.tolist(), None if first is None else first.tolist(),
+                                                                  table, stack, n_free)
+        assert not bad_len and not bad_page
+        assert d_table.cpu().tolist() == table
+        assert d_free.item() == n_free and d_stack.cpu().tolist() == stack
+        assert not rnd or granted.cpu().tolist() == g
+        held = [p for row in table for p in row if p >= 0]
+        assert len(set(held)) == len(held) and sorted(held + stack[:n_free]) == list(range(n_pages))
+        length = np.where(np.array(g) == 1, length, 0) if not partial else length
+        if not partial:                                                     # what was refused asks for nothing next time
+            eng.plan_pages(eng.i32(length), d_table, d_stack, d_free)
+            table, stack, n_free, *_ = R.plan_pages(pt, n_pages, 0, length.tolist(), None, table, stack, n_free)
+    assert eng.read_status() == 0
+
+
+def test_plan_pages_bad_values():
+    """Lengths outside the table, wrong entries and a wrong stack: flagged, nothing outside is touched, the others are served."""
+    pt, NP, n_pages = 4, 6, 10
+    eng = engine(page_tokens=pt, max_pages_per_seq=NP, n_pages=n_pages, max_batch=4, max_q=1)
+    cases = [
+        ([25, 8, -1, 4], None, [[-1] * NP for _ in range(4)], list(range(10)), 10),          # two rows are left alone
+        ([8, 8, 4, 4], [0, -1, 99, 0], [[-1] * NP for _ in range(4)], list(range(10)), 10),
+        ([0, 4, 4, 0], None, [[3, 10, 2 ** 31 - 1] + [-1] * 3, [-5] + [-1] * 5, [-1] * NP, [4] + [-1] * 5], [0, 1, 2] + [9] * 7, 3),
+        ([4, 4, 4, 0], None, [[-1] * NP for _ in range(4)], [5, -3, 10, 7] + [9] * 6, 4),     # ids that are none
+        ([0, 0, 0, 0], None, [[1, 2] + [-1] * 4, [1, 2] + [-1] * 4, [-1] * NP, [-1] * NP], list(range(10)), 8),    # given back twice
+        ([4, 0, 0, 0], None, [[-1] * NP for _ in range(4)], list(range(10)), 11),
+        ([4, 0, 0, 0], None, [[-1] * NP for _ in range(4)], list(range(10)), -2),
+    ]
+    for length, first, table, stack, n_free in cases:
+        eng.reset_status()
+        guard = eng.i32([[77] * NP] + table + [[77] * NP])
+        sg = eng.i32([77] + stack + [77])
+        free, granted = eng.i32([n_free]), eng.i32([9] * 4)
+        eng.plan_pages(eng.i32(length), guard[1:5], sg[1:11], free, granted, first=None if first is None else eng.i32(first))
+        t, s, n, g, bad_len, bad_page = R.plan_pages(pt, n_pages, 0, length, first, table, stack, n_free)
+        assert guard.cpu().tolist() == [[77] * NP] + t + [[77] * NP]
+        assert sg.cpu().tolist() == [77] + s + [77] and free.item() == n and granted.cpu().tolist() == g
+        assert eng.read_status() == (B.STATUS_BAD_LENGTH if bad_len else 0) | (B.STATUS_BAD_PAGE if bad_page else 0)
+
+
+@pytest.mark.parametrize("Bn,NP,pt", [(1, 1, 1), (1, 64, 16), (7, 9, 5), (300, 12, 32), (2100, 3, 7)])
+def test_slot_map(Bn, NP, pt):
+    rng = np.random.default_rng(Bn + NP)
+    n_pages = Bn * NP + 3
+    eng = engine(page_tokens=pt, max_pages_per_seq=NP, n_pages=n_pages, max_batch=Bn, max_q=1)
+    table = rng.permutation(n_pages)[:Bn * NP].reshape(Bn, NP)
+    table[rng.random((Bn, NP)) < 0.1] = -1
+    table[rng.random((Bn, NP)) < 0.02] = n_pages
+    start = rng.integers(0, NP * pt + 1, Bn)
+    end = np.where(rng.random(Bn) < 0.2, start - 1, np.minimum(NP * pt, start + rng.integers(0, NP * pt + 1, Bn))).clip(0)
+    total = int(np.maximum(0, end - start).sum())
+    for extra, s, e in ((0, start, end), (37, start, end), (-total // 2, start, end), (5, start - 2, end + 1)):
+        eng.reset_status()
+        cap = max(1, total + extra)
+        cu, slots = eng.i32([5] * (Bn + 1)), eng.i32([5] * (cap + 1))
+        eng.slot_map(eng.i32(s), eng.i32(e), eng.i32(table), cu, slots[:cap])
+        rc, rs, bad = R.slot_map(pt, n_pages, s.tolist(), e.tolist(), table.tolist(), cap)
+        assert cu.cpu().tolist() == rc and slots.cpu().tolist() == rs + [5]
+        assert eng.read_status() == (B.STATUS_BAD_LENGTH if bad else 0)
+
+
+# ------------------------------------------------------------------------------------------------ the 4-bit pool
+
+def bf16_values(rng, shape, kind):
+    x = rng.standard_normal(shape)
+    if kind == "ties":                                                      # quarters of a power of two: half-way points everywhere
+        x = rng.integers(-28, 29, shape) / 4 * 2.0 ** rng.integers(-3, 4, shape[:-1] + (1,))
+    if kind == "wide":
+        x = x * 2.0 ** rng.integers(-126, 121, shape)
+    if kind == "zeros":
+        x = np.where(rng.random(shape) < 0.9, 0, x) * (rng.random(shape[:-1] + (1,)) < 0.5)
+    x = torch.tensor(x, dtype=torch.float32).bfloat16()
+    if kind == "odd":
+        r = torch.tensor(rng.random(shape))
+        x[r < 0.02], x[(r > 0.02) & (r < 0.04)], x[r > 0.98] = float("inf"), float("-inf"), float("nan")
+    return x
+
+
+def record_of(eng, layer, slot, h):
+    """The record of the group that holds a slot of the 4-bit pool."""
+    pt, dh, hkv = eng.cfg.page_tokens, eng.cfg.head_dim, eng.cfg.n_kv_heads
+    at = ((layer * eng.n_pages4 + slot // pt) * hkv + h) * (pt // 32) + slot % pt // 32
+    return eng.kv4_pool[at * 34 * dh:(at + 1) * 34 * dh].cpu().numpy()
+
+
+@pytest.mark.parametrize("heads,pt", [("6/3x64", 32), ("6/3x64", 96), ("8/2x128", 64), ("5/5x128", 128)])
+@pytest.mark.parametrize("kind", ["normal", "ties", "wide", "zeros", "odd"])
+def test_store_and_load(heads, pt, kind):
+    """Records byte for byte, groups from runs of slots and from scattered ones, and the values read back elsewhere."""
+    rng = np.random.default_rng(pt + len(kind))
+    eng = engine(heads, layers=2, page_tokens=pt, max_pages_per_seq=4, n_pages=5, max_batch=1, max_q=1)
+    eng.attach_kv4(4)
+    _, hkv, dh = HEADS[heads]
+    for l in range(2):
+        for w in range(2):
+            eng.kv_slab(l, w).copy_(bf16_values(rng, (5, hkv, pt, dh), kind).to(eng.device))
+    eng.kv4_pool.fill_(0xA5)
+    before = [[eng.kv_slab(l, w).float().cpu().numpy().astype(np.float64) for w in range(2)] for l in range(2)]
+    # three groups: a run of slots, a run that is not aligned (or crosses a page), scattered ones; a fourth is padding
+    src = np.concatenate([np.arange(32), np.arange(32) + pt - 13, rng.permutation(3 * pt)[:32], np.full(32, -1)])
+    dst0 = rng.permutation(4 * pt // 32)[:3] * 32
+    dst = np.concatenate([np.arange(32) + d for d in dst0] + [np.full(32, -1)])
+    eng.kv4_store(eng.i32(src), eng.i32(dst))
+    assert eng.read_status() == (B.STATUS_NOT_FINITE if kind == "odd" else 0)
+    held = {}
+    for l in range(2):
+        for h in range(hkv):
+            for i in range(3):
+                s = src[32 * i:32 * i + 32]
+                k, v = (before[l][w][s // pt, h, s % pt] for w in range(2))
+                rec, rk, rv = R.records(k, v)
+                got = record_of(eng, l, int(dst0[i]), h)
+                got[:32 * dh] -= (((got[:32 * dh] & 15) == 8) * 8 + ((got[:32 * dh] >> 4) == 8) * 128).astype(np.uint8)   # -0 is 0
+                assert (got == rec).all(), (l, h, i, np.nonzero(got != rec)[0][:8])
+                held[l, h, i] = rk, rv
+    touched = {int(d) // 32 for d in dst0}
+    for g in range(4 * pt // 32):
+        if g not in touched:
+            assert (record_of(eng, 1, 32 * g, hkv - 1) == 0xA5).all()
+    # read back: whole groups in order, single positions in any order, into the last two pages
+    order = rng.permutation(96)[:2 * pt - 5]
+    back = np.concatenate([rng.permutation(2 * pt)[:len(order)] + 3 * pt, [-1]])
+    eng.reset_status()
+    eng.kv4_load(eng.i32(np.concatenate([dst[order], [-1]])), eng.i32(back))
+    assert eng.read_status() == 0
+    for l in range(2):
+        for w in range(2):
+            want = before[l][w].copy()
+            for o, t in zip(order, back):
+                for h in range(hkv):
+                    want[t // pt, h, t % pt] = held[l, h, o // 32][w][o % 32]
+            got = eng.kv_slab(l, w).float().cpu().numpy().astype(np.float64)
+            assert np.array_equal(got, want, equal_nan=True)
+
+
+def test_store_and_load_skip_what_is_wrong():
+    eng = engine(page_tokens=32, max_pages_per_seq=4, n_pages=3, max_batch=1, max_q=1)
+    eng.attach_kv4(2)
+    eng.kv_slab(0, 0).normal_()
+    eng.kv_slab(0, 1).normal_()
+    run = np.arange(32)
+    for src, dst, status in ((run, run, 0), (run + 65, run, 2), (run - 1, run, 2), (run, run + 1, 2), (run, run + 64, 2), (run, run[::-1], 2),
+                             (run, np.where(run == 3, -1, run), 2), (np.full(32, -1), run, 2), (run, np.full(32, -1), 0), (run, run - 2 ** 31, 2)):
+        eng.kv4_pool.fill_(0x5A)
+        eng.reset_status()
+        good = np.concatenate([src, run + 32]), np.concatenate([dst, run + 32])
+        eng.kv4_store(eng.i32(good[0]), eng.i32(good[1]))
+        assert eng.read_status() == status
+        assert (record_of(eng, 0, 32, 1) != 0x5A).any()                     # the other group is stored
+        assert (record_of(eng, 0, 0, 1) != 0x5A).any() == (status == 0 and dst[0] == 0)
+    eng.kv4_store(eng.i32(np.arange(64)), eng.i32(np.arange(64)))
+    for src, dst, status in ((run, run + 64, 0), (run + 33, run + 64, 2), (run, run + 65, 2), (np.where(run == 5, -1, run), run + 64, 2),
+                             (np.full(32, -1), np.full(32, -1), 0)):
+        pool = torch.zeros_like(eng.kv_slab(0, 0))
+        eng.kv_slab(0, 0)[2] = 0
+        eng.reset_status()
+        eng.kv4_load(eng.i32(src), eng.i32(dst))
+        assert eng.read_status() == status
+        n = int(((src >= 0) & (src < 64) & (dst >= 0) & (dst < 96)).sum())
+        assert int((eng.kv_slab(0, 0)[2, 0] != pool[2, 0]).any(-1).sum()) == n
+
+
+# ------------------------------------------------------------------------------------------------ attention
+
+class Cache:
+    """Dense float64 keys and values of a batch laid into an engine's pools, pages in random order; table entries of positions
+    that no row reads are -1."""
+
+    def __init__(self, heads, dtype, prefix, Q, valid, four, window, n_sink, pt, seed, mode=0, slack=0):
+        hq, hkv, dh = HEADS[heads]
+        rng = np.random.default_rng(seed)
+        Bn, self.Q, self.window, self.n_sink, self.dtype = len(prefix), Q, window, n_sink, dtype
+        NP = (max(prefix) + slack + Q + pt - 1) // pt
+        self.eng = eng = engine(heads, dtype, page_tokens=pt, max_pages_per_seq=NP, n_pages=Bn * NP + 1, max_batch=Bn, max_q=Q)
+        self.max_prefix = max(prefix) + slack
+        eng.set_kernel_mode(mode)
+        dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.prefix, self.valid = prefix, [Q] * Bn if valid is None else valid
+        self.n4 = [min(f, p) // 32 * 32 for f, p in zip(four, prefix)] if four else [0] * Bn
+        self.q = torch.tensor(rng.standard_normal((Bn, Q, hq, dh))).to(dt)
+        perm = rng.permutation(Bn * NP)
+        table, table4 = np.full((Bn, NP), -1), np.full((Bn, NP), -1)
+        if four:
+            eng.attach_kv4(Bn * NP + 1)
+            eng.kv4_pool.fill_(0xFF)                                        # NaN scales wherever nothing is stored
+        eng.kv_slab(0, 0).fill_(float("nan"))
+        eng.kv_slab(0, 1).fill_(float("nan"))
+        self.k, self.v = [], []
+        slab = [eng.kv_slab(0, w).cpu() for w in range(2)]
+        recs = eng.kv4_pool.cpu().numpy().reshape(Bn * NP + 1, hkv, pt // 32, 34 * dh) if four else None
+        for b, (p, n) in enumerate(zip(prefix, self.valid)):
+            k, v = (torch.tensor(rng.standard_normal((p + max(0, n), hkv, dh))).to(dt).double().numpy() for _ in range(2))
+            lo = max(0, p - window + 1) if window else 0
+            for j in range(len(k)):
+                if n_sink <= j < lo:
+                    continue
+                page, s = perm[b * NP + j // pt], j % pt
+                if j < self.n4[b]:
+                    table4[b, j // pt] = page
+                    if j % 32 == 0 or (j == lo and lo > n_sink):
+                        g = j // 32 * 32
+                        for h in range(hkv):
+                            rec, rk, rv = R.records(k[g:g + 32, h], v[g:g + 32, h])
+                            recs[page, h, s // 32] = rec
+                            k[g:g + 32, h], v[g:g + 32, h] = rk, rv
+                else:
+                    table[b, j // pt] = page
+                    slab[0][page, :, s], slab[1][page, :, s] = torch.tensor(k[j]).to(dt), torch.tensor(v[j]).to(dt)
+            self.k.append(k)
+            self.v.append(v)
+        for w in range(2):
+            eng.kv_slab(0, w).copy_(slab[w])
+        if four:
+            eng.kv4_pool.copy_(torch.from_numpy(recs.reshape(-1)))
+        self.table, self.table4 = table, table4
+        self.out = torch.full(self.q.shape, 7.0, dtype=dt, device=eng.device)
+        self.kw = dict(max_prefix_len=self.max_prefix, q_valid=None if valid is None else eng.i32(valid), window=window, n_sink=n_sink)
+        if four:
+            self.kw.update(len4=eng.i32(self.n4), table4=eng.i32(table4))
+
+    def run(self, out=None):
+        e = self.eng
+        e.attend(0, self.q.to(e.device), e.i32(self.prefix), e.i32(self.table), self.out if out is None else out, **self.kw)
+        return self
+
+    def check(self, rows=None):
+        got = self.out.double().cpu().numpy()
+        for b, (p, n) in enumerate(zip(self.prefix, self.valid)):
+            n = max(0, n)
+            q = self.q[b, :n].double().numpy()
+            ref, tol = R.attend(q, self.k[b], self.v[b], p, self.window, self.n_sink, self.dtype, self.n4[b])
+            bad = ~(np.abs(got[b, :n] - ref) <= tol)
+            assert not bad.any(), (b, np.argwhere(bad)[:4], float((np.abs(got[b, :n] - ref) / tol).max()))
+            assert (got[b, n:] == 7.0).all()
+        assert self.eng.read_status() == 0
+
+
+# heads, type, prefixes, rows, valid rows, positions in 4 bits (those that are whole groups), window, sinks, page
+CASES = [
+    ("6/3x64", "bf16", [0], 1, None, None, 0, 0, 16),
+    ("6/3x64", "bf16", [0], 1, None, None, 1, 0, 16),
+    ("6/3x64", "bf16", [5, 0, 200], 7, None, None, 3, 2, 8),
+    ("6/3x64", "f32", [5, 0, 200], 7, [7, 0, 3], None, 50, 2, 5),
+    ("4/4x64", "f32", [333, 300], 32, None, None, 100, 4, 16),
+    ("4/4x64", "bf16", [333, 300], 32, [-1, 31], None, 100, 40, 16),
+    ("4/4x64", "bf16", [130, 97], 33, None, None, 64, 33, 24),
+    ("8/2x128", "bf16", [1000, 31], 32, None, None, 128, 0, 32),
+    ("8/2x128", "bf16", [700], 64, [40], None, 31, 64, 7),
+    ("28/4x128", "bf16", [500, 450], 32, None, None, 200, 5, 64),
+    ("5/5x128", "bf16", [2000], 1, None, None, 0, 0, 64),
+    ("5/5x128", "bf16", [2000], 3, None, None, 1999, 1, 128),
+    ("6/3x64", "bf16", [32], 1, None, [32], 0, 0, 32),
+    ("6/3x64", "bf16", [300, 0, 64], 9, [9, 4, 0], [999] * 3, 0, 0, 32),
+    ("4/4x64", "bf16", [515, 640], 32, None, [999] * 2, 0, 0, 96),
+    ("4/4x64", "bf16", [515, 640], 32, None, [128, 640], 90, 40, 64),
+    ("8/2x128", "bf16", [1027], 32, None, [1024], 0, 0, 64),
+    ("8/2x128", "bf16", [1027, 900], 5, [5, 1], [999, 64], 300, 100, 32),
+    ("28/4x128", "bf16", [777, 700], 1, None, [999] * 2, 0, 0, 64),
+    ("28/4x128", "bf16", [640, 900], 33, [33, 20], [999] * 2, 257, 130, 128),
+    ("5/5x128", "bf16", [1500], 64, None, [9999], 0, 0, 64),
+    ("5/5x128", "bf16", [1500, 1], 1, None, [9999, 0], 1, 0, 64),
+    ("5/5x128", "bf16", [1500], 17, None, [9999], 7, 1500, 64),
+]
+
+
+@pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
+@pytest.mark.parametrize("i", range(len(CASES)))
+def test_attend(i, mode):
+    Cache(*CASES[i], seed=100 + i, mode=mode).run().check()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("Q", [1, 32])
+def test_attend_long(four, Q):
+    """Many parts along the keys, one sequence much longer than the others, a host bound that is longer still."""
+    Cache("8/2x128", "bf16", [9000, 40, 4097], Q, None, [9999] * 3 if four else None, 0, 0, 64, seed=5 + Q, slack=700).run().check()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
+def test_what_is_not_read_does_not_reach_a_row(four, mode):
+    """Infinities and NaN in keys and values that some rows read and others do not: a row's output is what it would be without
+    those it does not read (and NaN where it reads a NaN)."""
+    c = Cache("6/3x64", "bf16", [200], 32, None, [64] if four else None, 60, 70, 16 if not four else 32, seed=1, mode=mode)
+    clean = c.run().out.clone()
+    c.check()
+    # position 150 is read by rows whose p - 60 < 150: rows 0 .. 9 (p = 200 + j); 145 by rows 0 .. 4
+    pt = c.eng.cfg.page_tokens
+    for pos, val in ((150, float("nan")), (145, float("inf"))):
+        page = c.table[0, pos // pt]
+        row = c.eng.kv_slab(0, 1)[page, 1, pos % pt]
+        keep = row.clone()
+        row.fill_(val)
+        got = c.run().out
+        row.copy_(keep)
+        last = pos + 59 - 200                                               # the last row that reads it is at pos + 59
+        assert not torch.isfinite(got[0, :last + 1, 2:4]).any()             # its two query heads
+        assert torch.equal(got[0, last + 1:], clean[0, last + 1:])
+        assert torch.equal(got[0, :, :2], clean[0, :, :2]) and torch.equal(got[0, :, 4:], clean[0, :, 4:])
+    page = c.table[0, 160 // pt]
+    c.eng.kv_slab(0, 0)[page, 0, 160 % pt] = float("nan")                   # a key: rows 0 .. 19, heads 0 and 1
+    got = c.run().out
+    assert torch.isnan(got[0, :20, :2]).all() and torch.equal(got[0, 20:], clean[0, 20:])
+    assert c.eng.read_status() == 0
+
+
+@pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
+def test_scores_without_a_finite_one(mode):
+    """Scores of -infinity weigh nothing; a row with no other is NaN, as is one with a +infinity or a NaN query."""
+    c = Cache("6/3x64", "bf16", [40], 4, None, None, 0, 0, 16, seed=3, mode=mode)
+    c.q[0, :, 0] = 1.0
+    k = c.eng.kv_slab(0, 0)
+    for pos in range(44):
+        k[c.table[0, pos // 16], 0, pos % 16, 0] = float("-inf")
+    got = c.run().out
+    assert torch.isnan(got[0, :, 0]).all()
+    k[c.table[0, 2], 0, 1] = 0.25                                           # one key is finite
+    got = c.run().out
+    v = c.eng.kv_slab(0, 1)[c.table[0, 2], 0, 1]
+    assert torch.equal(got[0, :, 0], v.expand(4, 64))
+    c.q[0, 1, 5] = float("nan")
+    c.q[0, 2, 5] = float("inf")
+    got = c.run().out
+    assert torch.isnan(got[0, 1:3, 5]).all() and torch.isfinite(got[0, :, 4]).all() and torch.isfinite(got[0, [0, 3], 5]).all()
+
+
+@pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
+def test_nan_query_over_4_bits(mode):
+    c = Cache("8/2x128", "bf16", [256], 4, None, [256], 0, 0, 32, seed=4, mode=mode)
+    c.q[0, 1, 5, 100] = float("nan")
+    c.q[0, 2, 3, 7] = float("inf")
+    c.q[0, 3, 0] = 0.0
+    c.q[0, 3, 1] *= 2.0 ** -100
+    got = c.run().out
+    assert torch.isnan(got[0, 1, 5]).all() and torch.isnan(got[0, 2, 3]).all()
+    rest = torch.ones(4, 8, dtype=torch.bool)
+    rest[1, 5] = rest[2, 3] = False
+    assert torch.isfinite(got[0].cpu()[rest]).all()
+    ref, tol = R.attend(c.q[0, 3:].double().numpy(), c.k[0][:260], c.v[0], 256, 0, 0, "bf16", 256)
+    assert (np.abs(got[0, 3:].double().cpu().numpy() - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
+def test_bad_values_on_the_device(four, mode):
+    """Prefix lengths beyond the host's bound and pages outside the pool are flagged; keys of such pages are left out; entries
+    that map nothing that is read are not looked at."""
+    pt = 32
+    c = Cache("6/3x64", "bf16", [190, 150], 8, None, [64, 64] if four else None, 100, 20, pt, seed=8, mode=mode)
+    c.table[0, 0 if four else 1] = 12345                                    # (not read: in 4 bits / between sinks and window)
+    c.run().check()
+    c.table4[1, 1], keep = -9, c.table4[1, 1]
+    if four:
+        c.kw["table4"] = c.eng.i32(c.table4)                                # positions 32 .. 63 of sequence 1: window starts at 51
+        c.run()
+        assert c.eng.read_status() == B.STATUS_BAD_PAGE
+        c.eng.reset_status()
+        see = [j for j in range(158) if j < 20 or j >= 64]                  # what is left of the keys, for the row at 150 (51 .. 63 lost)
+        ref, tol = R.attend(c.q[1, :1].double().numpy(), c.k[1][see], c.v[1][see], len(see) - 1, 0, 0, "bf16", 64)
+        assert (np.abs(c.out[1, :1].double().cpu().numpy() - ref) <= tol).all()
+        c.table4[1, 1] = keep
+        c.kw["table4"] = c.eng.i32(c.table4)
+    keep = c.table[1, 4]
+    c.table[1, 4] = c.eng.cfg.n_pages                                       # positions 128 .. 157 of sequence 1
+    c.run()
+    assert c.eng.read_status() == B.STATUS_BAD_PAGE
+    see = [j for j in range(158) if j < 20 or 51 <= j < 128]
+    ref, tol = R.attend(c.q[1, :1].double().numpy(), c.k[1][see], c.v[1][see], len(see) - 1, 0, 0, "bf16", 64 if four else 0)
+    assert (np.abs(c.out[1, :1].double().cpu().numpy() - ref) <= tol).all()
+    c.table[1, 4] = keep
+    for prefix, kw in (([191, 150], {}), ([-1, 150], {})):
+        c.eng.reset_status()
+        c.eng.attend(0, c.q.to(c.eng.device), c.eng.i32(prefix), c.eng.i32(c.table), c.out, **{**c.kw, "max_prefix_len": 190, **kw})
+        assert c.eng.read_status() & B.STATUS_BAD_LENGTH
+        c.eng.reset_status()
+    if four:
+        for n4 in ([65, 64], [-32, 64], [224, 64]):
+            c.run(torch.empty_like(c.out))
+            c.eng.reset_status()
+            c.kw["len4"] = c.eng.i32(n4)
+            c.run(torch.empty_like(c.out))
+            assert c.eng.read_status() & B.STATUS_BAD_LENGTH
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_offsets_beyond_32_bits(four):
+    """Pages whose bytes lie past 4 GiB of a slab (the 4-bit pool: past 4 GiB of it)."""
+    pt, hkv, dh = 64, 4, 128
+    ms = dataclasses.replace(SMALL, n_q_heads=8, n_kv_heads=hkv, head_dim=dh)
+    n_pages = (1 << 32) // (hkv * pt * dh * 2) + 8 if not four else 16
+    eng = H.make_engine(ms, synth.Weights(ms, 0), pack=False, page_tokens=pt, max_pages_per_seq=4, n_pages=n_pages, max_batch=1, max_q=2)
+    rng = np.random.default_rng(2)
+    k, v = (torch.tensor(rng.standard_normal((194, hkv, dh))).bfloat16() for _ in range(2))
+    pages = [n_pages - 1 - i for i in range(4)]
+    for j in range(194):
+        eng.kv_slab(0, 0)[pages[j // pt], :, j % pt] = k[j].to(eng.device)
+        eng.kv_slab(0, 1)[pages[j // pt], :, j % pt] = v[j].to(eng.device)
+    kw, kk, vv = {}, k.double().numpy(), v.double().numpy()
+    if four:
+        n4 = (1 << 32) // (hkv * 2 * 34 * dh) + 8
+        eng.attach_kv4(n4)
+        t4 = eng.i32([[n4 - 3, n4 - 1, n4 - 5, -1]])
+        cu, src, dst = eng.i32([0, 0]), eng.i32([0] * 192), eng.i32([0] * 192)
+        eng.slot_map(eng.i32([0]), eng.i32([192]), eng.i32([pages]), cu, src)
+        eng.slot_map(eng.i32([0]), eng.i32([192]), t4, cu, dst, kv4=True)
+        eng.kv4_store(src, dst)
+        kw = dict(len4=eng.i32([192]), table4=t4)
+        for h in range(hkv):
+            for g in range(0, 192, 32):
+                _, kk[g:g + 32, h], vv[g:g + 32, h] = R.records(kk[g:g + 32, h], vv[g:g + 32, h])
+    q = torch.tensor(rng.standard_normal((1, 2, 8, dh))).bfloat16()
+    for mode in (0, 1):
+        eng.set_kernel_mode(mode)
+        out = torch.empty_like(q, device=eng.device)
+        eng.attend(0, q.to(eng.device), eng.i32([192]), eng.i32([pages]), out, max_prefix_len=192, **kw)
+        ref, tol = R.attend(q[0].double().numpy(), kk, vv, 192, 0, 0, "bf16", 192 if four else 0)
+        assert (np.abs(out[0].double().cpu().numpy() - ref) <= tol).all()
+    assert eng.read_status() == 0
+
+
+def test_binding_checks():
+    c = Cache("6/3x64", "bf16", [40], 4, None, None, 0, 0, 16, seed=3)
+    e, q = c.eng, c.q.to(c.eng.device)
+    good = dict(max_prefix_len=40)
+    for bad in (q.float(), q[:, :, :3], q.transpose(1, 2).contiguous().transpose(1, 2), c.q):
+        with pytest.raises(ValueError):
+            e.attend(0, bad, e.i32([40]), e.i32(c.table), c.out, **good)
+    with pytest.raises(ValueError):
+        e.attend(0, q, e.i32([40, 1]), e.i32(c.table), c.out, **good)
+    with pytest.raises(ValueError):
+        e.attend(0, q, e.i32([40]).long(), e.i32(c.table), c.out, **good)
+    with pytest.raises(B.DllmError):
+        e.attend(1, q, e.i32([40]), e.i32(c.table), c.out, **good)
+    with pytest.raises(B.DllmError):
+        e.slot_map(e.i32([0]), e.i32([1]), e.i32(c.table), e.i32([0, 0]), e.i32([0]), kv4=True)
+    with pytest.raises(B.DllmError):
+        e.attach_kv4(4)                                                      # pages of 16
+
+
+def test_streams_and_replays():
+    """The calls of a turn on a stream of their own, and captured into a graph that is replayed with eager work between: every
+    replay gives the eager result."""
+    eng = engine("8/2x128", page_tokens=32, max_pages_per_seq=12, n_pages=64, max_batch=3, max_q=4)
+    eng.attach_kv4(40)
+    for w in range(2):
+        eng.kv_slab(0, w).normal_()
+    q = torch.randn(3, 4, 8, 128, device=eng.device).bfloat16()
+    length, len4 = eng.i32([300, 96, 37]), eng.i32([288, 96, 32])
+    total = eng.i32([304, 100, 41])
+    zero = eng.i32([0] * 3)
+
+    def fresh():
+        return dict(t=eng.i32([[-1] * 12] * 3), s=eng.i32(list(range(64))[::-1]), n=eng.i32([64]), t4=eng.i32([[-1] * 12] * 3),
+                    s4=eng.i32(list(range(40))), n4=eng.i32([40]), cu=eng.i32([0] * 4), a=eng.i32([0] * 448), d=eng.i32([0] * 448),
+                    out=torch.zeros_like(q))
+
+    def turn(x):
+        eng.plan_pages(total, x["t"], x["s"], x["n"])
+        eng.plan_pages(len4, x["t4"], x["s4"], x["n4"], kv4=True)
+        eng.slot_map(zero, len4, x["t"], x["cu"], x["a"])
+        eng.slot_map(zero, len4, x["t4"], x["cu"], x["d"], kv4=True)
+        eng.kv4_store(x["a"], x["d"])
+        eng.attend(0, q, length, x["t"], x["out"], max_prefix_len=300, len4=len4, table4=x["t4"], window=200, n_sink=40)
+    eager = fresh()
+    turn(eager)
+    torch.cuda.synchronize()
+    side, other = torch.cuda.Stream(), fresh()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        turn(other)
+    side.synchronize()
+    graph, captured, init = torch.cuda.CUDAGraph(), fresh(), fresh()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            turn(captured)
+    for _ in range(4):
+        for k in captured:
+            captured[k].copy_(init[k])
+        eng.kv4_pool.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in eager:
+            assert torch.equal(captured[k], eager[k]) and torch.equal(other[k], eager[k]), k
+        (q.float() * 2).sum().item()
+    assert eng.read_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ the step
+
+def test_step_without_a_view_is_the_step():
+    ms = dataclasses.replace(SMALL, n_layers=2, d_model=128, d_ff=96, vocab=320, mask_id=319)
+    eng = H.make_engine(ms, synth.Weights(ms, 1), page_tokens=32, max_pages_per_seq=6, n_pages=12, max_batch=2, max_q=32, max_tokens=256)
+    rng = np.random.default_rng(1)
+    bt, pl = eng.i32(H.identity_table(eng, 2)), eng.i32([100, 77])
+    eng.prefill_kv(eng.i32(rng.integers(0, 300, 177)), eng.i32([0, 100, 177]), bt, total_tokens=177, max_seqlen=100)
+    toks = eng.i32(np.where(rng.random((2, 32)) < 0.7, 319, 5))
+    res = []
+    for call in (lambda *o: eng.denoise_step(toks, pl, bt, *o, max_prefix_len=100), lambda *o: eng.denoise_step_view(toks, pl, bt, *o, max_prefix_len=100),
+                 lambda *o: eng.denoise_step_view(toks, pl, bt, *o, max_prefix_len=100, n_sink=3)):
+        o = torch.zeros(2, 32, dtype=torch.int32, device=eng.device), torch.zeros(2, 32, device=eng.device), torch.zeros(2, 32, device=eng.device)
+        call(*o)
+        res.append(o)
+    assert all(torch.equal(a, b) for r in res[1:] for a, b in zip(res[0], r))
+
+
+def view_step(ms, weights, block, cache, prefix, window, n_sink, n_valid, widen, store):
+    """The forward of a step (the oracle's layers) whose rows read what the view lets them: logits of the first n_valid rows."""
+    block = np.asarray(block)[:n_valid]
+    x = O._f64(np.asarray(weights["tok_emb"])[block], widen)
+    for l in range(ms.n_layers):
+        lw = weights.layer(l)
+        q, k, v = O.layer_qkv(ms, lw, x, np.arange(n_valid) + prefix, widen, store)
+        o, _ = R.attend(q, np.concatenate([cache[l][0], k]), np.concatenate([cache[l][1], v]), prefix, window, n_sink, "f32")
+        x = O.layer_finish(ms, lw, x, o, widen, store)
+    return O.head_logits(weights, x, widen, store)
+
+
+@pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
+@pytest.mark.parametrize("dtype,Q,valid", [("bf16", 32, [32, 32, 32]), ("bf16", 16, [16, 9, 0]), ("bf16", 48, None), ("f32", 16, [16, 16, 5]), ("f32", 40, None)])
+def test_turn_of_a_long_sequence(dtype, Q, valid, mode):
+    """Everything together: pages planned for the prompts, prefill, the complete positions put away in 4 bits (bfloat16), their
+    pages given back, then steps that read all of it, and sinks and a window of it."""
+    ms = dataclasses.replace(SMALL, n_layers=2, d_model=256, n_q_heads=4, n_kv_heads=2, d_ff=128, vocab=512, mask_id=511, dtype=dtype, lm_head_scale=8.0)
+    w = synth.Weights(ms, 3)
+    pt, NP, n_pages, prompt = 32, 9, 24, [230, 64, 121]
+    eng = H.make_engine(ms, w, page_tokens=pt, max_pages_per_seq=NP, n_pages=n_pages, max_batch=3, max_q=Q, max_tokens=512)
+    eng.set_kernel_mode(mode)
+    rng = np.random.default_rng(11)
+    table, stack, n_free = eng.i32([[-1] * NP] * 3), eng.i32(rng.permutation(n_pages)), eng.i32([n_pages])
+    eng.plan_pages(eng.i32([p + Q for p in prompt]), table, stack, n_free)
+    toks = rng.integers(0, 511, sum(prompt))
+    eng.prefill_kv(eng.i32(toks), eng.i32(np.cumsum([0] + prompt)), table, n_cache=None, total_tokens=sum(prompt), max_seqlen=max(prompt))
+    host = table.cpu().numpy()
+    cache = [[[H.gather_cache(eng, host[b], prompt[b], l, x).astype(np.float64) for x in (0, 1)] for l in range(2)] for b in range(3)]
+    kw, n4 = {}, [0, 0, 0]
+    if dtype == "bf16":
+        n4 = [p // 32 * 32 for p in prompt]
+        eng.attach_kv4(16)
+        table4, s4, f4, len4 = eng.i32([[-1] * NP] * 3), eng.i32(rng.permutation(16)), eng.i32([16]), eng.i32(n4)
+        granted, cu, src, dst = eng.i32([0] * 3), eng.i32([0] * 4), eng.i32([0] * 512), eng.i32([0] * 512)
+        eng.plan_pages(len4, table4, s4, f4, granted, kv4=True)
+        assert granted.cpu().tolist() == [1, 1, 1]
+        eng.slot_map(eng.i32([0] * 3), len4, table, cu, src)
+        eng.slot_map(eng.i32([0] * 3), len4, table4, cu, dst, kv4=True)
+        eng.kv4_store(src, dst)
+        kw = dict(len4=len4, table4=table4)
+        for b in range(3):
+            for l in range(2):
+                for g in range(0, n4[b], 32):
+                    for h in range(2):
+                        k, v = cache[b][l]
+                        _, k[g:g + 32, h], v[g:g + 32, h] = R.records(k[g:g + 32, h], v[g:g + 32, h])
+        eng.plan_pages(eng.i32([p + Q for p in prompt]), table, stack, n_free, first=len4)
+        for l in range(2):                                                  # nothing of what was put away is left in the other pool
+            for x in (0, 1):
+                slab = eng.kv_slab(l, x)
+                for p in stack.cpu().tolist()[:n_free.item()]:
+                    slab[p] = float("nan")
+    pl = eng.i32(prompt)
+    for window, n_sink in ((0, 0), (70, 5)):
+        if window:                                                          # what lies between is given back too
+            eng.plan_pages(eng.i32([p + Q for p in prompt]), table, stack, n_free, first=eng.i32([max(n, p - window + 1) for n, p in zip(n4, prompt)]),
+                           keep_head=0 if kw else n_sink)
+        block = np.where(rng.random((3, Q)) < 0.7, 511, rng.integers(0, 511, (3, Q))).astype(np.int32)
+        cand = torch.zeros(3, Q, dtype=torch.int32, device=eng.device)
+        conf, ent = torch.zeros(3, Q, device=eng.device), torch.zeros(3, Q, device=eng.device)
+        eng.denoise_step_view(eng.i32(block), pl, table, cand, conf, ent, max_prefix_len=max(prompt), q_valid=None if valid is None else eng.i32(valid),
+                              window=window, n_sink=n_sink, **kw)
+        assert eng.read_status() == 0
+        for b in range(3):
+            n = Q if valid is None else valid[b]
+            masked = block[b, :n] == 511
+            if n == 0:
+                continue
+            logits = view_step(ms, w, block[b], cache[b], prompt[b], window, n_sink, n, synth.as_float if dtype == "bf16" else None, H.STORE[dtype])
+            r = {"logits": logits, "cand": O.confidence(logits, 511)[0]}
+            H.check_step_outputs(ms, r, masked, cand[b, :n].cpu().numpy(), conf[b, :n].cpu().numpy(), ent[b, :n].cpu().numpy(), dtype)
+            assert (cand[b].cpu().numpy()[n:] == block[b, n:]).all() and (conf[b, n:] == 1).all()
