@@ -11,8 +11,13 @@ struct AttendArgs {
   const void *k, *v;        // slabs of the layer
   const uint8_t* kv4;       // records of the layer
   int B, Q, Hq, Hkv, max_prefix, window, n_sink;
-  int pt, max_pages, n_pages, n_pages4;
+  int pt, pt_shift, max_pages, n_pages, n_pages4;   // pt_shift: log2(pt) if that is a power of two of at least 32, else -1
   int32_t* status;
+  // k_attend
+  int n_rg_wg, kspl;        // row groups of a workgroup, its waves along the keys of each
+  int n_parts;              // workgroups along the keys; > 1: partial results, merged by k_attend_merge
+  float scale_log2;         // log2(e) / sqrt(dh)
+  float *part_o, *part_ml;  // [rows, n_parts, dh], [rows, n_parts, 2]
 };
 
 // The keys of sequence b: n_q rows at positions pl .. pl + n_q - 1 read keys [0, kv_len), those below n4 in 4 bits.
@@ -139,6 +144,516 @@ __global__ __launch_bounds__(256) void k_attend_any(const AttendArgs a, int dh) 
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
 }
 
+// ==========================================================================================
+// bfloat16 models with pages of a multiple of 8 tokens.
+//
+// One wave owns 16 * QT rows (head in group, token) of a (sequence, kv head) and walks blocks of keys: 128 of them in 4 bits, then 32
+// in bfloat16.  Both kinds compute S^T = K Q^T and O^T = V^T P^T with K rows and V^T rows (channels) as the first operand of a
+// 16-row matrix instruction, so that a query's scores, statistics and sums stay in the lanes of its column and the scores' layout is
+// the second product's operand as it stands (K rows are handed out to match).
+//
+// 4 bits: v_mfma_scale_f32_16x16x128 multiplies the codes as they lie in memory, with the power of two of every 32 values along k as the
+// instruction's own scale; nothing is unpacked.  Its other operand is e4m3: a query row (scaled by a power of two) enters as hi + lo / 16, two
+// e4m3 values that together hold the 8 significant bits of a bfloat16 exactly (but for channels 2^14 below the row's largest, whose
+// error is 2^-21 of that one); a probability enters the same way, which rounds it to 8 bits (relative 2^-8 at most, 2^-10 on average).
+// Operand layouts (lane l, c = l % 16, g = l / 16): the 4-bit operand holds row c, k = 32g .. +31; the e4m3 one column c, bytes 0-15: k =
+// 16g .. +15, bytes 16-31: k = 64 + 16g .. +15; the scale of the block of k 32x .. +31 is taken from lane group x.  D holds column c,
+// rows 4g .. 4g+3.  So row 4a + i of score tile t is given key 64 (t/4) + 16a + 4 (t%4) + i, and tile t's four scores are bytes 4t ..
+// 4t+3 of the second product's operand.  With 64 channels k holds them twice, against hi and lo of the query.
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+template <int SEL>
+__device__ __forceinline__ f32x4 mfma4(u32x4 a, i32x8 b, f32x4 c, uint32_t scale_a, uint32_t scale_b) {
+  const i32x8 av = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, b, c, 4, 0, SEL, (int)scale_a, 0, (int)scale_b);
+}
+__device__ __forceinline__ f32x4 mfma4_sel(int sel, u32x4 a, i32x8 b, f32x4 c, uint32_t scale_a, uint32_t scale_b) {
+  switch (sel) {   // (a constant once the loops are unrolled)
+    case 0: return mfma4<0>(a, b, c, scale_a, scale_b);
+    case 1: return mfma4<1>(a, b, c, scale_a, scale_b);
+    case 2: return mfma4<2>(a, b, c, scale_a, scale_b);
+    default: return mfma4<3>(a, b, c, scale_a, scale_b);
+  }
+}
+// four floats -> four e4m3 (hi) and what they leave out, times 16, in e4m3 (lo)
+__device__ __forceinline__ void e4m3_pair(float x0, float x1, float x2, float x3, int& hi, int& lo) {
+  int h = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
+  h = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, h, true);
+  const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+  s16x2 l = {0, 0};
+  l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x0 - a[0], x1 - a[1], 0.0625f, false);
+  l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x2 - b[0], x3 - b[1], 0.0625f, true);
+  hi = h;
+  lo = __builtin_bit_cast(int, l);
+}
+
+// Probabilities are kept 2^8 times too large: the largest is then near the top of e4m3, and the sums divide it out again.
+constexpr float P_SHIFT = 8.0f;
+
+// Online softmax of NT score tiles (log2 units after scale_log2); s becomes the probabilities.  A row that has seen no key but
+// masked ones keeps the maximum -inf and weights 0.
+template <int NT, int DT, int QT>
+__device__ __forceinline__ void attend_softmax(f32x4 (&s)[NT][QT], float scale_log2, float (&m_run)[QT], float (&l_run)[QT], f32x4 (&oacc)[DT][QT]) {
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float mx = s[0][t][0];
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[x][t][i]);
+    mx = rows_max(mx);
+    const float m_new = fmaxf(m_run[t], mx * scale_log2);
+    const float base = m_new > -DEV_INF ? m_new : 0.f;
+    if (__builtin_amdgcn_ballot_w64(m_new > m_run[t]) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(m_run[t] - base);
+      l_run[t] *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) oacc[d][t] = oacc[d][t] * alpha;
+      m_run[t] = m_new;
+    }
+    const float off = P_SHIFT - base;
+    float ps = 0.f;
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[x][t][i], scale_log2, off));
+        s[x][t][i] = e;
+        ps += e;
+      }
+    l_run[t] += ps;
+  }
+}
+
+template <int DH, int QT>
+__global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
+  constexpr int KK = DH / 32, DT = DH / 16, UN = DT * QT;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int rw = w / a.kspl, kw = w - rw * a.kspl;             // row group and place along the keys inside the workgroup
+  const int rg = blockIdx.y * a.n_rg_wg + rw;
+  const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv;
+  const int G = a.Hq / a.Hkv;
+  const AttendSeq sq = attend_seq(a, b);
+  if (sq.bad && threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+  const int n_q = sq.n_q, R = n_q * G, kv_len = sq.kv_len, n4 = sq.n4;
+  if (blockIdx.y * a.n_rg_wg * 16 * QT >= R) return;           // (the whole workgroup)
+  const bool active = rg * 16 * QT < R;
+  const int U = a.n_parts * a.kspl, unit = blockIdx.z * a.kspl + kw;
+
+  // the lane's queries, and what the wave's rows read: [0, n_head) and [lo, kv_len), all of it from lo_all on
+  int64_t row_out[QT];
+  int row_in[QT], wlo[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = rg * 16 * QT + t * 16 + c, rr = min(r, R - 1);
+    const int hg = rr / n_q, j = rr - hg * n_q;
+    row_in[t] = (b * a.Q + j) * a.Hq + kvh * G + hg;
+    row_out[t] = r < R ? row_in[t] : -1;
+    wlo[t] = a.window > 0 ? sq.pl + j - a.window : -1;         // keys above it are read
+  }
+  int lo = 0, lo_all = 0, n_head = 0;
+  if (a.window > 0) {
+    const int r0 = min(rg * 16 * QT, R - 1), r1 = min(rg * 16 * QT + 16 * QT, R) - 1;
+    const bool one = r0 / n_q == r1 / n_q;
+    lo = max(0, sq.pl + (one ? r0 % n_q : 0) - a.window + 1);
+    lo_all = max(0, sq.pl + (one ? r1 % n_q : n_q - 1) - a.window + 1);
+    n_head = min(a.n_sink, lo);
+  }
+  auto read_all = [&](int k0, int k1) { return k1 <= a.n_sink || k0 >= lo_all; };     // every row reads keys k0 .. k1 - 1
+  auto read_any = [&](int k0, int k1) { return k0 < n_head || k1 > lo; };             // some row may
+
+  f32x4 oacc[DT][QT];
+  float m_run[QT], l_run[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m_run[t] = -DEV_INF;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) oacc[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  bool bad = false;
+  const bf16_t* const q = (const bf16_t*)a.q;
+  int n_blk4 = 0;
+
+  // ---- keys in 4 bits, blocks of 128: those of the head, then those from lo on
+  if (n4 > 0 && active) {
+    const int first = min(lo, n4) >> 7, last = (n4 + 127) >> 7;
+    const int n_b = lo < n4 ? last - first : 0;
+    int n_a = (min(n_head, n4) + 127) >> 7;
+    if (n_b > 0) n_a = min(n_a, first);
+    n_blk4 = n_a + n_b;
+    i32x8 qh[QT], ql[DH == 128 ? QT : 1];
+    uint32_t qs[QT];                                            // scale bytes: hi, lo in the next byte (DH 64: the lane's own)
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const bf16_t* p = q + (int64_t)row_in[t] * DH + 16 * g;
+      uint32_t x[DH / 8];
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) {
+        const u32x4 u = *(const u32x4*)(p + 64 * i), v = *(const u32x4*)(p + 64 * i + 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[8 * i + e] = u[e]; x[8 * i + 4 + e] = v[e]; }
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < DH / 8; ++i) top = max(top, max(x[i] & 0x7fffu, (x[i] >> 16) & 0x7fffu));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+      const uint32_t e = max(top >> 7, 12u);                    // the largest channel goes to 2^7 .. 2^8
+      const float f = __uint_as_float((261u - e) << 23);
+      int h[DH / 16], l[DH / 16];
+#pragma unroll
+      for (int i = 0; i < DH / 16; ++i)
+        e4m3_pair(__uint_as_float(x[2 * i] << 16) * f, __uint_as_float(x[2 * i] & 0xffff0000u) * f, __uint_as_float(x[2 * i + 1] << 16) * f,
+                  __uint_as_float(x[2 * i + 1] & 0xffff0000u) * f, h[i], l[i]);
+      if constexpr (DH == 128) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { qh[t][i] = h[i]; ql[t][i] = l[i]; }
+        qs[t] = (e - 7) | (e - 11) << 8;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { qh[t][i] = h[i]; qh[t][4 + i] = l[i]; }
+        qs[t] = g < 2 ? e - 7 : e - 11;
+      }
+    }
+    const int gpp = a.pt >> 5;                                  // groups of 32 a page
+    const int32_t* const table = a.table4 + (int64_t)b * a.max_pages;
+    const int gk = (c >> 3), kin = 16 * ((c >> 2) & 1) + (c & 3), gch = DH == 128 ? g : g & 1;
+    const int k_off = kin * (DH / 2) + gch * 16, ks_off = 32 * DH + (((c >> 2) & 1) * 4 + (c & 3)) * (DH / 8) + gch * 4;
+    const int v_off = 16 * DH + c * 16, vs_off = 33 * DH + c * (DH / 16);
+    auto block_at = [&](int i) { return i < n_a ? i : first + (i - n_a); };
+    // records of the groups whose keys (two halves) and values the lane loads: table entries first, a block ahead
+    // (no branch around a load: it would wait for all of them)
+    auto page_of = [&](int grp) { return a.pt_shift >= 0 ? grp >> (a.pt_shift - 5) : grp / gpp; };
+    auto entry = [&](int grp) { const int pi = page_of(grp), e = table[min(pi, a.max_pages - 1)]; return pi < a.max_pages ? e : -1; };
+    auto record = [&](int grp, int page, bool& ok) -> const uint8_t* {
+      ok = (uint32_t)page < (uint32_t)a.n_pages4;
+      return a.kv4 + (((int64_t)(ok ? page : 0) * a.Hkv + kvh) * gpp + (grp - page_of(grp) * gpp)) * (34 * DH);
+    };
+    int e0, e1, ev;
+    {
+      const int g0 = block_at(min(unit, n_blk4 - 1)) << 2;
+      e0 = entry(g0 + gk); e1 = entry(g0 + 2 + gk); ev = entry(g0 + g);
+    }
+    for (int i = unit; i < n_blk4; i += U) {
+      const int g0 = block_at(i) << 2, k0 = g0 << 5;
+      bool ok0, ok1, okv;
+      const uint8_t *r0 = record(g0 + gk, e0, ok0), *r1 = record(g0 + 2 + gk, e1, ok1), *rv = record(g0 + g, ev, okv);
+      u32x4 kf[8], vf[DT];
+      uint32_t ks[2], vs[DT / 4];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) kf[t] = *(const u32x4*)((t < 4 ? r0 : r1) + k_off + (t & 3) * 4 * (DH / 2));
+      ks[0] = *(const uint32_t*)(r0 + ks_off);
+      ks[1] = *(const uint32_t*)(r1 + ks_off);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[d] = *(const u32x4*)(rv + v_off + d * 256);
+#pragma unroll
+      for (int d = 0; d < DT / 4; ++d) vs[d] = *(const uint32_t*)(rv + vs_off + d * 4);
+      {
+        const int g1 = block_at(min(i + U, n_blk4 - 1)) << 2;
+        e0 = entry(g1 + gk); e1 = entry(g1 + 2 + gk); ev = entry(g1 + g);
+      }
+      // groups of which no key is read, or that cannot be: anything may lie there
+      const int kg = k0 + 32 * g;
+      const bool want = kg < n4 && read_any(kg, kg + 32), dead = !(want && okv);
+      bad |= want && !okv;
+      const uint64_t dead_m = __builtin_amdgcn_ballot_w64(dead);
+      f32x4 s[8][QT];
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+          acc = mfma4_sel(t & 3, kf[t], qh[x], acc, ks[t >> 2], qs[x]);
+          if constexpr (DH == 128) acc = mfma4_sel(t & 3, kf[t], ql[x], acc, ks[t >> 2], qs[x] >> 8);
+          s[t][x] = acc;
+        }
+      if (dead_m != 0 || !read_all(k0, k0 + 128)) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const bool gone = (dead_m >> (16 * (2 * (t >> 2) + (g >> 1)))) & 1;
+#pragma unroll
+          for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = k0 + 64 * (t >> 2) + 16 * g + 4 * (t & 3) + e;
+              if (gone || !(key < a.n_sink || key > wlo[x])) s[t][x][e] = -DEV_INF;
+            }
+        }
+        if (dead) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) vf[d] = u32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int d = 0; d < DT / 4; ++d) vs[d] = 0x7f7f7f7fu;
+        }
+      }
+      attend_softmax<8, DT, QT>(s, a.scale_log2, m_run, l_run, oacc);
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        i32x8 ph, pl;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          int h, l;
+          e4m3_pair(s[t][x][0], s[t][x][1], s[t][x][2], s[t][x][3], h, l);
+          ph[t] = h;
+          pl[t] = l;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          oacc[d][x] = mfma4_sel(d & 3, vf[d], ph, oacc[d][x], vs[d >> 2], 127);
+          oacc[d][x] = mfma4_sel(d & 3, vf[d], pl, oacc[d][x], vs[d >> 2], 123);
+        }
+      }
+    }
+  }
+
+  // ---- keys in bfloat16, blocks of 32, two at a time; the units go on behind the ones that took the last blocks of 128
+  if (active) {
+    const int f16 = n4 >> 5;
+    const int sB = max(lo, n4) >> 5, n_b = ((kv_len + 31) >> 5) - sB;
+    const int n_a = min(max(0, ((n_head + 31) >> 5) - f16), sB - f16), n_blk = n_a + n_b;
+    auto block_at = [&](int i) { return i < n_a ? f16 + i : sB + (i - n_a); };
+    const bf16_t *kslab = (const bf16_t*)a.k, *vslab = (const bf16_t*)a.v;
+    const int32_t* const table = a.table + (int64_t)b * a.max_pages;
+    u32x4 qf[QT][KK];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) qf[t][kk] = *(const u32x4*)(q + (int64_t)row_in[t] * DH + kk * 32 + g * 8);
+    struct Blk { u32x4 kf[2][KK], vf[DT]; bool dead; };
+    auto page_of = [&](int key) { return a.pt_shift >= 0 ? key >> a.pt_shift : key / a.pt; };
+    auto entry = [&](int key) { const int pi = page_of(key), e = table[min(pi, a.max_pages - 1)]; return pi < a.max_pages ? e : -1; };
+    auto issue = [&](int kb, int ek, int ev, Blk& x) {
+      const int k0 = kb << 5, key_k = k0 + 8 * (c >> 2), key_v = k0 + 8 * g;     // (8 consecutive keys lie in one page)
+      const bool okk = (uint32_t)ek < (uint32_t)a.n_pages, okv = (uint32_t)ev < (uint32_t)a.n_pages;
+      const bool want = key_v < kv_len && read_any(key_v, key_v + 8);
+      x.dead = !(want && okv);
+      bad |= want && !okv;
+      const bf16_t* kp = kslab + (((int64_t)(okk ? ek : 0) * a.Hkv + kvh) * a.pt + (key_k - page_of(key_k) * a.pt) + (c & 3)) * DH + g * 8;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) x.kf[tt][kk] = *(const u32x4*)(kp + tt * 4 * DH + kk * 32);
+      const bf16_t* vp = vslab + (((int64_t)(okv ? ev : 0) * a.Hkv + kvh) * DH + c) * a.pt + (key_v - page_of(key_v) * a.pt);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) x.vf[d] = *(const u32x4*)(vp + (int64_t)d * 16 * a.pt);
+    };
+    auto zero_keys = [&](u32x4 (&vf)[DT], int k0, auto gone) {                   // V of the lane's keys for which gone(key)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = k0 + 8 * g + 2 * e;
+        const uint32_t m = (gone(key) ? 0u : 0xffffu) | (gone(key + 1) ? 0u : 0xffff0000u);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vf[d][e] &= m;
+      }
+    };
+    auto compute = [&](int kb, Blk& x) {
+      const int k0 = kb << 5;
+      f32x4 s[2][QT];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) acc = mfma16(x.kf[tt][kk], qf[t][kk], acc);
+          s[tt][t] = acc;
+        }
+      bool apart = false;                                       // some rows do not read a value that is not finite
+      if (__builtin_amdgcn_ballot_w64(x.dead) != 0 || k0 + 32 > kv_len || !read_all(k0, k0 + 32)) {
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = k0 + 8 * g + 4 * tt + e;
+              if (x.dead || key >= kv_len || !(key < a.n_sink || key > wlo[t])) s[tt][t][e] = -DEV_INF;
+            }
+        zero_keys(x.vf, k0, [&](int key) { return x.dead || key >= kv_len; });
+        if (!read_all(k0, k0 + 32)) {
+          bool odd = false;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t v = x.vf[d][e];
+              odd |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+            }
+          apart = __builtin_amdgcn_ballot_w64(odd) != 0;
+        }
+      }
+      attend_softmax<2, DT, QT>(s, a.scale_log2, m_run, l_run, oacc);
+      u32x4 ph[QT], pl[QT];
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = s[e >> 1][t][(e & 1) * 2], p1 = s[e >> 1][t][(e & 1) * 2 + 1];
+          const uint32_t h = pack_bf16x2(p0, p1);
+          ph[t][e] = h;
+          pl[t][e] = pack_bf16x2(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
+        }
+      if (!apart) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            oacc[d][t] = mfma16(x.vf[d], ph[t], oacc[d][t]);
+            oacc[d][t] = mfma16(x.vf[d], pl[t], oacc[d][t]);
+          }
+      } else {
+        // 0 * NaN is NaN: one query at a time, with the values it does not read taken out
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          for (int cc = 0; cc < 16; ++cc) {
+            const int wl = __shfl(wlo[t], cc, 64);
+            u32x4 v[DT], h, l;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) v[d] = x.vf[d];
+            zero_keys(v, k0, [&](int key) { return !(key < a.n_sink || key > wl); });
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { h[e] = c == cc ? ph[t][e] : 0u; l[e] = c == cc ? pl[t][e] : 0u; }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              f32x4 o = mfma16(v[d], h, oacc[d][t]);
+              o = mfma16(v[d], l, o);
+              if (c == cc) oacc[d][t] = o;                      // (the other columns got 0 * NaN)
+            }
+          }
+      }
+    };
+    int i = unit - n_blk4 % U;
+    if (i < 0) i += U;
+    int ka = 0, va = 0, kb2 = 0, vb = 0;
+    auto entries = [&](int i, int& ek, int& ev) {
+      const int k0 = block_at(max(0, min(i, n_blk - 1))) << 5;
+      ek = entry(k0 + 8 * (c >> 2));
+      ev = entry(k0 + 8 * g);
+    };
+    entries(i, ka, va);
+    entries(i + U, kb2, vb);
+    for (; i < n_blk; i += 2 * U) {
+      const bool two = i + U < n_blk;
+      Blk x, y;
+      issue(block_at(i), ka, va, x);
+      issue(block_at(two ? i + U : i), two ? kb2 : ka, two ? vb : va, y);   // (a repeat of the first block's loads)
+      entries(i + 2 * U, ka, va);
+      entries(i + 3 * U, kb2, vb);
+      compute(block_at(i), x);
+      if (two) compute(block_at(i + U), y);
+    }
+  }
+
+  // ---- results: the lane holds query column c, channels d*16 + 4g + i
+  float l_red[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float l = l_run[t];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    l_red[t] = l;
+  }
+  auto store = [&](int d, int t, f32x4 v, float m, float l) {
+    const int64_t ro = row_out[t];
+    if (ro < 0) return;
+    const int ch = d * 16 + 4 * g;
+    if (a.n_parts > 1) {
+      const int64_t slot = ro * a.n_parts + blockIdx.z;
+      *(f32x4*)(a.part_o + slot * DH + ch) = v;
+      if (d == 0 && g == 0) { a.part_ml[slot * 2] = m; a.part_ml[slot * 2 + 1] = l; }
+      return;
+    }
+    const float inv = 1.0f / l;                                 // (no finite score: 0 / 0)
+    const int tok = (int)(ro / a.Hq), head = (int)(ro - (int64_t)tok * a.Hq);
+    const int64_t at = a.out_mt > 0 ? frag_offset(tok, head * DH + ch, a.out_mt) : ro * DH + ch;
+    *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
+  };
+  if (a.kspl == 1) {
+    if (active)
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) store(d, t, oacc[d][t], m_run[t], l_red[t]);
+  } else {
+    // the waves of a row group bring their sums to a common maximum and hand each other slices of the channels through LDS
+    const int KS = a.kspl;
+    float* sm_m = (float*)smem + rw * KS * QT * 32;             // [KS][QT][16] maxima, then sums
+    float* sm_l = sm_m + KS * QT * 16;
+    f32x4* sm_o = (f32x4*)(smem + 4 * QT * 32 * sizeof(float)) + (int64_t)rw * UN * (KS - 1) * 64;   // [UN][KS - 1][64]
+    if (active && g == 0) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) { sm_m[(kw * QT + t) * 16 + c] = m_run[t]; sm_l[(kw * QT + t) * 16 + c] = l_red[t]; }
+    }
+    __syncthreads();
+    float m_all[QT], l_all[QT];
+    if (active) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        float mx = -DEV_INF;
+        for (int k = 0; k < KS; ++k) mx = fmaxf(mx, sm_m[(k * QT + t) * 16 + c]);
+        const float base = mx > -DEV_INF ? mx : 0.f;
+        float ls = 0.f;
+        for (int k = 0; k < KS; ++k) ls = fmaf(sm_l[(k * QT + t) * 16 + c], __builtin_amdgcn_exp2f(sm_m[(k * QT + t) * 16 + c] - base), ls);
+        m_all[t] = mx;
+        l_all[t] = ls;
+        const float f = __builtin_amdgcn_exp2f(m_run[t] - base);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          oacc[d][t] = oacc[d][t] * f;
+          const int u = d * QT + t, own = u & (KS - 1);         // (KS is 2 or 4)
+          if (own != kw) sm_o[(u * (KS - 1) + ((kw - own - 1) & (KS - 1))) * 64 + lane] = oacc[d][t];
+        }
+      }
+    }
+    __syncthreads();
+    if (active) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const int u = d * QT + t;
+          if ((u & (KS - 1)) != kw) continue;
+          f32x4 v = oacc[d][t];
+          for (int k = 0; k < KS - 1; ++k) v = v + sm_o[(u * (KS - 1) + k) * 64 + lane];
+          store(d, t, v, m_all[t], l_all[t]);
+        }
+      // (statistics of the parts go with channel tile 0, whose wave they belong to)
+    }
+  }
+  if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
+}
+
+// Partial results of a row: four channels a lane.
+template <int DH>
+__global__ __launch_bounds__(256) void k_attend_merge(const AttendArgs a, int64_t n_rows) {
+  constexpr int LR = DH / 4;
+  const int64_t row = (int64_t)blockIdx.x * (256 / LR) + threadIdx.x / LR;
+  if (row >= n_rows) return;
+  const int ch = threadIdx.x % LR * 4;
+  const int tok = (int)(row / a.Hq), head = (int)(row - (int64_t)tok * a.Hq), b = tok / a.Q;
+  const int qv = a.q_valid ? a.q_valid[b] : a.Q;
+  if (tok - b * a.Q >= qv) return;                               // (no partials of rows that are not part of the call)
+  const float* ml = a.part_ml + row * a.n_parts * 2;
+  const float* po = a.part_o + row * a.n_parts * DH + ch;
+  float mx = -DEV_INF;
+  for (int p = 0; p < a.n_parts; ++p) mx = fmaxf(mx, ml[2 * p]);
+  const float base = mx > -DEV_INF ? mx : 0.f;
+  float den = 0.f;
+  f32x4 num = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < a.n_parts; ++p) {
+    const float f = __builtin_amdgcn_exp2f(ml[2 * p] - base);
+    den = fmaf(ml[2 * p + 1], f, den);
+    num = num + *(const f32x4*)(po + (int64_t)p * DH) * f;
+  }
+  const float inv = 1.0f / den;
+  const int64_t at = a.out_mt > 0 ? frag_offset(tok, head * DH + ch, a.out_mt) : row * DH + ch;
+  *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv));
+}
+
 hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int layer, const void* q, void* o, int out_mt) {
   const dllm_config& f = c->cfg;
   const KVView kv = pool_view(c, g, layer);
@@ -151,7 +666,32 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
   a.B = g.B; a.Q = g.Q; a.Hq = f.n_q_heads; a.Hkv = f.n_kv_heads; a.max_prefix = g.max_kv - g.Q;
   a.window = g.view->window; a.n_sink = g.view->n_sink;
   a.pt = f.page_tokens; a.max_pages = f.max_pages_per_seq; a.n_pages = f.n_pages; a.n_pages4 = c->n_pages4;
+  a.pt_shift = -1;
+  for (int sh = 5; sh < 31; ++sh) if (f.page_tokens == 1 << sh) a.pt_shift = sh;
   a.status = WSM(c, status, int32_t);
+  if (f.dtype == DLLM_BF16 && c->kernel_mode == 0 && f.page_tokens % 8 == 0 && c->map.attn_rows > 0) {
+    const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, c->map.attn_rows);
+    a.n_rg_wg = p.n_rg_wg; a.kspl = p.kspl; a.n_parts = p.n_parts;
+    a.scale_log2 = 1.4426950408889634f / sqrtf((float)f.head_dim);
+    a.part_o = WSM(c, attn_part, float);
+    a.part_ml = a.part_o + (size_t)c->map.attn_rows * f.head_dim;
+    const dim3 grid(g.B * f.n_kv_heads, p.n_chunks, p.n_parts);
+    const int threads = 64 * p.n_rg_wg * p.kspl;
+    const size_t lds = p.kspl == 1 ? 0 : (size_t)4 * p.qt * 32 * 4 + (size_t)p.n_rg_wg * (f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;
+    if (f.head_dim == 128) {
+      if (p.qt == 1) k_attend<128, 1><<<grid, threads, lds, s>>>(a);
+      else k_attend<128, 2><<<grid, threads, lds, s>>>(a);
+    } else {
+      if (p.qt == 1) k_attend<64, 1><<<grid, threads, lds, s>>>(a);
+      else k_attend<64, 2><<<grid, threads, lds, s>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.n_parts == 1) return e;
+    const int64_t rows = (int64_t)g.T * f.n_q_heads;
+    if (f.head_dim == 128) k_attend_merge<128><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a, rows);
+    else k_attend_merge<64><<<(unsigned)((rows + 15) / 16), 256, 0, s>>>(a, rows);
+    return hipGetLastError();
+  }
   if (f.dtype == DLLM_BF16) k_attend_any<bf16_t><<<dim3(g.T, f.n_q_heads), 256, 0, s>>>(a, f.head_dim);
   else k_attend_any<float><<<dim3(g.T, f.n_q_heads), 256, 0, s>>>(a, f.head_dim);
   return hipGetLastError();

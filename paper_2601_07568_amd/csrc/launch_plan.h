@@ -277,4 +277,35 @@ inline bool gt_qkv_fused(int cus, int M, int dq, int dkv, int dh, int K, int max
   return fused.us <= split.us + 10.0 + (4.0 * split.splits + 2.0) * M * (double)nw / 2.5e6;
 }
 
+// ---- attention over parts of the cache (k_attend)
+struct AttendPlan {
+  int qt;                   // 16-row tiles of a wave
+  int n_rg_wg, n_chunks;    // row groups (16 * qt rows) of a workgroup, workgroups along them
+  int kspl, n_parts;        // waves along the keys of a row group in a workgroup, workgroups along the keys
+};
+// max_kv: most keys of a sequence; four: most of them are in 4 bits
+inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int Q, int max_kv, int window, int n_sink, bool four, int64_t part_rows) {
+  AttendPlan p{};
+  const int G = n_q_heads / n_kv_heads, rows = Q * G;
+  p.qt = rows <= 16 ? 1 : 2;
+  const int n_rg = (rows + 16 * p.qt - 1) / (16 * p.qt);
+  p.n_rg_wg = n_rg >= 3 ? 4 : n_rg;
+  p.n_chunks = (n_rg + p.n_rg_wg - 1) / p.n_rg_wg;
+  // most keys that a row group reads, in blocks of its walk
+  int64_t keys = max_kv;
+  if (window > 0 && (int64_t)window + Q + n_sink < keys) keys = (int64_t)window + Q + n_sink;
+  const int64_t blocks = four ? keys / 128 + 2 : keys / 32 + 1;
+  // two waves a SIMD; one wave may take a whole block
+  const int64_t groups = (int64_t)B * n_kv_heads * p.n_chunks * p.n_rg_wg;
+  int64_t units = (int64_t)cus * 8 / groups;
+  if (units > blocks) units = blocks;
+  if (units < 1) units = 1;
+  p.kspl = 4 / p.n_rg_wg;
+  if (p.kspl > units) p.kspl = units >= 2 ? 2 : 1;
+  p.n_parts = (int)((units + p.kspl - 1) / p.kspl);
+  if (p.n_parts > ATTN_MAX_SPLITS) p.n_parts = ATTN_MAX_SPLITS;
+  while (p.n_parts > 1 && (int64_t)p.n_parts * B * Q * n_q_heads > part_rows) --p.n_parts;
+  return p;
+}
+
 }  // namespace dllm
