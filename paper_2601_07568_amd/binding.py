@@ -167,13 +167,14 @@ class Engine:
         self.workspace = torch.empty(ws_bytes + 256, dtype=torch.uint8, device=self.device)
         self._ws_off = (-self.workspace.data_ptr()) % 256
         self.kv_pool = torch.zeros(max(kv_bytes, 1), dtype=torch.uint8, device=self.device)
+        self._lib, self._home = L, self.kv_pool.device
         self.ctx = C.c_void_p()
         rc = L.dllm_create(C.byref(self.ctx), C.byref(self.cfg), C.byref(self._w), self.kv_pool.data_ptr(),
                            kv_bytes, self.workspace.data_ptr() + self._ws_off, ws_bytes)
         if rc != DLLM_OK:
             raise DllmError(rc)
         self._check(L.dllm_reset_status(self.ctx, self._stream()))
-        self.packed = None
+        self.packed = self.kv4_pool = None
         if ms.dtype == "bf16" and pack:
             pb = L.dllm_packed_weight_bytes(C.byref(self.cfg))
             self.packed = torch.empty(pb + 256, dtype=torch.uint8, device=self.device)
@@ -206,13 +207,10 @@ class Engine:
         """View of the pool as [n_pages, n_kv_heads, page_tokens, head_dim] of layer, which (0=K, 1=V);
         the V slab is stored [.., head_dim, page_tokens] and is returned transposed back."""
         c = self.cfg
-        es = 2 if self.ms.dtype == "bf16" else 4
         n = c.n_pages * c.n_kv_heads * c.page_tokens * c.head_dim
-        off = (layer * 2 + which) * n * es
-        flat = self.kv_pool[off:off + n * es].view(self.tdtype)
-        if which == 1:
-            return flat.view(c.n_pages, c.n_kv_heads, c.head_dim, c.page_tokens).transpose(2, 3)
-        return flat.view(c.n_pages, c.n_kv_heads, c.page_tokens, c.head_dim)
+        off, pt, dh = (layer * 2 + which) * n, c.page_tokens, c.head_dim
+        strides = (c.n_kv_heads * pt * dh, pt * dh, 1, pt) if which == 1 else (c.n_kv_heads * pt * dh, pt * dh, dh, 1)
+        return self.kv_pool.view(self.tdtype).as_strided((c.n_pages, c.n_kv_heads, pt, dh), strides, off)
 
     # -- the calls of include/dllm.h
     def prefill_kv(self, tokens, cu_seqlens, block_table, n_cache=None, *, total_tokens, max_seqlen):
@@ -357,82 +355,99 @@ class Engine:
                                              _ptr(conf), _ptr(entropy)))
 
     # -- long caches
-    def _dev(self, name, t, dtype, *shape, optional=False):
-        """Pointer of a contiguous tensor of this device; the calls below check what the library cannot see."""
-        if t is None and optional:
+    def _dev(self, name, t, dtype, shape):
+        """Address of a contiguous tensor of this device; the calls below check what the library cannot see.  None: NULL."""
+        if t is None:
             return None
-        if t.device != self.kv_pool.device or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {list(shape)} on {self.kv_pool.device}, got {t.dtype} "
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != self._home:
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {list(shape)} on {self._home}, got {t.dtype} "
                              f"{list(t.shape)} with strides {list(t.stride())} on {t.device}")
-        return C.c_void_p(t.data_ptr())
+        return t.data_ptr()
 
     def _call(self, fn, *args):
         """One library call on the current stream of the engine's device, with that device current."""
-        with self.torch.cuda.device(self.device):
-            self._check(fn(self.ctx, self._stream(), *args))
+        cuda, index = self.torch.cuda, self._home.index
+        stream = self.torch._C._cuda_getCurrentRawStream(index)     # (the stream object of the public call costs 2 us)
+        if cuda.current_device() == index:
+            rc = fn(self.ctx, stream, *args)
+        else:
+            with cuda.device(index):
+                rc = fn(self.ctx, stream, *args)
+        if rc != DLLM_OK:
+            self._check(rc)
 
     def attach_kv4(self, n_pages4: int):
         """A pool of n_pages4 pages in 4 bits beside the engine's (0: takes it away again)."""
-        self.kv4_pool = None
         if n_pages4 == 0:
-            self._check(lib().dllm_kv4_attach(self.ctx, None, 0, 0))
+            self._check(self._lib.dllm_kv4_attach(self.ctx, None, 0, 0))
+            self.kv4_pool = None
             return
-        n = lib().dllm_kv4_pool_bytes(C.byref(self.cfg), n_pages4)
+        n = self._lib.dllm_kv4_pool_bytes(C.byref(self.cfg), n_pages4)
         if n == 0 and self.ms.n_layers > 0:
             raise DllmError(DLLM_ESHAPE, "(no 4-bit cache of this model, page size or number of pages)")
         pool = self.torch.zeros(max(n, 1), dtype=self.torch.uint8, device=self.device)   # (the allocator aligns to 512 bytes)
-        self._check(lib().dllm_kv4_attach(self.ctx, C.c_void_p(pool.data_ptr()), n, n_pages4))
+        self._check(self._lib.dllm_kv4_attach(self.ctx, pool.data_ptr(), n, n_pages4))
         self.kv4_pool, self.n_pages4 = pool, n_pages4
 
     def _pool(self, kv4):
-        if kv4 and getattr(self, "kv4_pool", None) is None:
+        if kv4 and self.kv4_pool is None:
             raise DllmError(DLLM_EINVAL, "(no 4-bit pool attached)")
         return (POOL_KV4, self.n_pages4) if kv4 else (POOL_KV, self.cfg.n_pages)
 
     def plan_pages(self, length, block_table, free_pages, n_free, granted=None, *, first=None, keep_head=0, kv4=False):
-        i32, (pool, n_pages), B = self.torch.int32, self._pool(kv4), length.numel()
-        self._call(lib().dllm_plan_pages, pool, B, keep_head, self._dev("length", length, i32, B),
-                   self._dev("first", first, i32, B, optional=True),
-                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq),
-                   self._dev("free_pages", free_pages, i32, n_pages), self._dev("n_free", n_free, i32, 1),
-                   self._dev("granted", granted, i32, B, optional=True))
+        i32, (pool, n_pages), B, dev = self.torch.int32, self._pool(kv4), length.numel(), self._dev
+        self._need(length=length, block_table=block_table, free_pages=free_pages, n_free=n_free)
+        self._call(self._lib.dllm_plan_pages, pool, B, keep_head, dev("length", length, i32, (B,)), dev("first", first, i32, (B,)),
+                   dev("block_table", block_table, i32, (B, self.cfg.max_pages_per_seq)), dev("free_pages", free_pages, i32, (n_pages,)),
+                   dev("n_free", n_free, i32, (1,)), dev("granted", granted, i32, (B,)))
 
     def slot_map(self, start, end, block_table, cu, slots, *, kv4=False):
-        i32, (pool, _), B = self.torch.int32, self._pool(kv4), start.numel()
-        self._call(lib().dllm_slot_map, pool, B, slots.numel(), self._dev("start", start, i32, B), self._dev("end", end, i32, B),
-                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq), self._dev("cu", cu, i32, B + 1),
-                   self._dev("slots", slots, i32, slots.numel()))
+        i32, pool, B, dev = self.torch.int32, self._pool(kv4)[0], start.numel(), self._dev
+        self._need(end=end, block_table=block_table, cu=cu, slots=slots)
+        n = slots.numel()
+        self._call(self._lib.dllm_slot_map, pool, B, n, dev("start", start, i32, (B,)), dev("end", end, i32, (B,)),
+                   dev("block_table", block_table, i32, (B, self.cfg.max_pages_per_seq)), dev("cu", cu, i32, (B + 1,)),
+                   dev("slots", slots, i32, (n,)))
 
     def kv4_store(self, src_slots, dst_slots):
         i32, n = self.torch.int32, src_slots.numel()
-        self._call(lib().dllm_kv4_store, n, self._dev("src_slots", src_slots, i32, n), self._dev("dst_slots", dst_slots, i32, n))
+        self._need(dst_slots=dst_slots)
+        self._call(self._lib.dllm_kv4_store, n, self._dev("src_slots", src_slots, i32, (n,)), self._dev("dst_slots", dst_slots, i32, (n,)))
 
     def kv4_load(self, src_slots, dst_slots):
         i32, n = self.torch.int32, src_slots.numel()
-        self._call(lib().dllm_kv4_load, n, self._dev("src_slots", src_slots, i32, n), self._dev("dst_slots", dst_slots, i32, n))
+        self._need(dst_slots=dst_slots)
+        self._call(self._lib.dllm_kv4_load, n, self._dev("src_slots", src_slots, i32, (n,)), self._dev("dst_slots", dst_slots, i32, (n,)))
+
+    def _need(self, **tensors):
+        for name, t in tensors.items():
+            if t is None:
+                raise ValueError(f"{name}: a tensor is needed")
 
     def _view(self, B, window, n_sink, len4, table4):
         i32 = self.torch.int32
-        return C.byref(CacheView(window, n_sink, self._dev("len4", len4, i32, B, optional=True),
-                                 self._dev("table4", table4, i32, B, self.cfg.max_pages_per_seq, optional=True)))
+        return C.byref(CacheView(window, n_sink, self._dev("len4", len4, i32, (B,)),
+                                 self._dev("table4", table4, i32, (B, self.cfg.max_pages_per_seq))))
 
     def attend(self, layer, q, prefix_len, block_table, out, *, max_prefix_len, q_valid=None, window=0, n_sink=0, len4=None,
                table4=None):
-        i32, (B, Q) = self.torch.int32, q.shape[:2]
-        shape = (B, Q, self.cfg.n_q_heads, self.cfg.head_dim)
-        self._call(lib().dllm_attend, layer, B, Q, max_prefix_len, self._dev("q", q, self.tdtype, *shape),
-                   self._dev("prefix_len", prefix_len, i32, B), self._dev("q_valid", q_valid, i32, B, optional=True),
-                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq),
-                   self._view(B, window, n_sink, len4, table4), self._dev("out", out, self.tdtype, *shape))
+        i32, dev, cfg, (B, Q) = self.torch.int32, self._dev, self.cfg, q.shape[:2]
+        self._need(prefix_len=prefix_len, block_table=block_table, out=out)
+        shape = (B, Q, cfg.n_q_heads, cfg.head_dim)
+        self._call(self._lib.dllm_attend, layer, B, Q, max_prefix_len, dev("q", q, self.tdtype, shape),
+                   dev("prefix_len", prefix_len, i32, (B,)), dev("q_valid", q_valid, i32, (B,)),
+                   dev("block_table", block_table, i32, (B, cfg.max_pages_per_seq)),
+                   self._view(B, window, n_sink, len4, table4), dev("out", out, self.tdtype, shape))
 
     def denoise_step_view(self, q_tokens, prefix_len, block_table, cand, conf, entropy=None, *, max_prefix_len, q_valid=None,
                           window=0, n_sink=0, len4=None, table4=None):
-        i32, f32, (B, Q) = self.torch.int32, self.torch.float32, q_tokens.shape
-        self._call(lib().dllm_denoise_step_view, B, Q, max_prefix_len, self._dev("q_tokens", q_tokens, i32, B, Q),
-                   self._dev("prefix_len", prefix_len, i32, B), self._dev("q_valid", q_valid, i32, B, optional=True),
-                   self._dev("block_table", block_table, i32, B, self.cfg.max_pages_per_seq),
-                   self._view(B, window, n_sink, len4, table4), self._dev("cand", cand, i32, B, Q),
-                   self._dev("conf", conf, f32, B, Q), self._dev("entropy", entropy, f32, B, Q, optional=True))
+        i32, f32, dev, (B, Q) = self.torch.int32, self.torch.float32, self._dev, q_tokens.shape
+        self._need(prefix_len=prefix_len, block_table=block_table, cand=cand, conf=conf)
+        self._call(self._lib.dllm_denoise_step_view, B, Q, max_prefix_len, dev("q_tokens", q_tokens, i32, (B, Q)),
+                   dev("prefix_len", prefix_len, i32, (B,)), dev("q_valid", q_valid, i32, (B,)),
+                   dev("block_table", block_table, i32, (B, self.cfg.max_pages_per_seq)),
+                   self._view(B, window, n_sink, len4, table4), dev("cand", cand, i32, (B, Q)),
+                   dev("conf", conf, f32, (B, Q)), dev("entropy", entropy, f32, (B, Q)))
 
     def debug_logits(self, q_tokens, prefix_len, block_table, *, max_prefix_len):
         B, Q = q_tokens.shape

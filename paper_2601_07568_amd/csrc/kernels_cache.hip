@@ -11,8 +11,8 @@ struct PlanArgs {
   int B, max_pages, pt, n_pages, keep_head;
   const int32_t *length, *first;
   int32_t *table, *stack, *n_free, *granted, *status;
-  int32_t *rel, *need, *hdr;      // workspace: pages given back and missing per sequence, then their prefix sums; hdr[0] pages that were
-                                  // free, hdr[1] free once everything given back has been pushed
+  int32_t *rel, *need, *hdr;      // workspace: pages that sequences give back (~n: and wrong entries) and miss (-1: a row that is left
+                                  // alone); hdr[0] pages that were free, hdr[1] free once everything given back has been pushed
 };
 
 struct PlanRow { int n_head, lo, hi; bool ok; };   // entries [0, n_head) and [lo, hi) are needed
@@ -27,78 +27,63 @@ __device__ inline PlanRow plan_row(const PlanArgs& a, int b) {
 }
 __device__ inline bool plan_needed(const PlanRow& r, int p) { return p < r.n_head || (p >= r.lo && p < r.hi); }
 
-// One wave: pages that sequence b gives back (those of the pool) and entries it misses; need -1: a row that is left alone.
+__device__ inline int plan_given(int rel) { return rel < 0 ? ~rel : rel; }
+
+// One wave: pages that sequence b gives back and entries it misses.
 __device__ inline void plan_count(const PlanArgs& a, int b, int lane) {
   const PlanRow r = plan_row(a, b);
   int rel = 0, need = 0;
+  bool wrong = false;
   for (int p = lane; p < a.max_pages && r.ok; p += 64) {
     const int e = a.table[(int64_t)b * a.max_pages + p];
     const bool n = plan_needed(r, p);
     rel += e >= 0 && e < a.n_pages && !n;
+    wrong |= e >= a.n_pages && !n;
     need += e < 0 && n;
   }
   for (int o = 32; o > 0; o >>= 1) { rel += __shfl_xor(rel, o, 64); need += __shfl_xor(need, o, 64); }
+  const bool any = __builtin_amdgcn_ballot_w64(wrong) != 0;
   if (lane == 0) {
-    a.rel[b] = rel;
+    a.rel[b] = any ? ~rel : rel;
     a.need[b] = r.ok ? need : -1;
     if (!r.ok) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
   }
 }
-// One workgroup of 1024: exclusive prefix sums of rel and, for the granted, of need (-1: not granted); the stack's size.
-__device__ inline void plan_scan(const PlanArgs& a, int tid) {
-  __shared__ int32_t w_rel[16];
-  __shared__ int64_t w_need[16];
-  __shared__ int32_t s_rel;
-  __shared__ int64_t s_need;
+// Sums over a workgroup of NT threads; every thread gets the total and the sum of the threads before it.
+template <int NT, typename T>
+__device__ inline T block_scan(T v, int tid, T* sm, T& total) {
   const int lane = tid & 63, w = tid >> 6;
-  const int nf_in = a.n_free[0], nf = min(max(nf_in, 0), a.n_pages);
-  if (tid == 0) { s_rel = 0; s_need = 0; }
+  T x = v;
+  for (int o = 1; o < 64; o <<= 1) { const T y = __shfl_up(x, o, 64); if (lane >= o) x += y; }
   __syncthreads();
-  // pages given back first: the grants depend on their number
-  for (int b0 = 0; b0 < a.B; b0 += 1024) {
-    const int b = b0 + tid, v = b < a.B ? a.rel[b] : 0;
-    int x = v;
-    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o, 64); if (lane >= o) x += y; }
-    if (lane == 63) w_rel[w] = x;
-    __syncthreads();
-    int before = s_rel;
-    for (int i = 0; i < w; ++i) before += w_rel[i];
-    if (b < a.B) a.rel[b] = before + x - v;
-    __syncthreads();
-    if (tid == 1023) s_rel = before + x;
-    __syncthreads();
-  }
-  const int64_t sum = (int64_t)nf + s_rel;
-  const int top = (int)(sum < a.n_pages ? sum : a.n_pages);
-  for (int b0 = 0; b0 < a.B; b0 += 1024) {
-    const int b = b0 + tid, v = b < a.B ? a.need[b] : 0;
-    int64_t x = v > 0 ? v : 0;
-    for (int o = 1; o < 64; o <<= 1) { const int64_t y = __shfl_up(x, o, 64); if (lane >= o) x += y; }
-    if (lane == 63) w_need[w] = x;
-    __syncthreads();
-    int64_t upto = s_need + x;
-    for (int i = 0; i < w; ++i) upto += w_need[i];
-    const bool ok = v == 0 || (v > 0 && upto <= top);
-    if (b < a.B) {
-      a.need[b] = ok ? (int32_t)(v == 0 ? 0 : upto - v) : -1;
-      if (a.granted) a.granted[b] = ok ? 1 : 0;
-    }
-    __syncthreads();
-    if (tid == 1023) s_need = upto;
-    __syncthreads();
-  }
-  if (tid == 0) {
-    a.hdr[0] = nf;
-    a.hdr[1] = top;
-    if (nf != nf_in) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
-    if (sum > top) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
-  }
+  if (lane == 63) sm[w] = x;
+  __syncthreads();
+  T before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) { if (i < w) before += sm[i]; total += sm[i]; }
+  return before + x - v;
+}
+// Pages that are free before the call, and once everything given back is on the stack.
+__device__ inline int plan_free(const PlanArgs& a, bool report) {
+  const int n = a.n_free[0], nf = min(max(n, 0), a.n_pages);
+  if (report && nf != n) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+  return nf;
+}
+__device__ inline int plan_top(const PlanArgs& a, int nf, int64_t rel, bool report) {
+  const int64_t sum = nf + rel;
+  if (report && sum > a.n_pages) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
+  return (int)(sum < a.n_pages ? sum : a.n_pages);
+}
+// What the grants say of sequence b, which misses `need` entries where those before it miss `before`: the first place from the
+// top that its pages are popped from, -1: it gets nothing.
+__device__ inline int plan_grant(int need, int64_t before, int top) {
+  return need < 0 ? -1 : (need == 0 ? 0 : (before + need <= top ? (int)before : -1));
 }
 // One wave: what sequence b gives back goes onto the stack.
-__device__ inline void plan_release(const PlanArgs& a, int b, int lane) {
+__device__ inline void plan_release(const PlanArgs& a, int b, int lane, int at) {
   const PlanRow r = plan_row(a, b);
   if (!r.ok) return;
-  int at = a.hdr[0] + a.rel[b];
   bool bad = false;
   for (int p0 = 0; p0 < a.max_pages; p0 += 64) {
     const int p = p0 + lane;
@@ -114,12 +99,9 @@ __device__ inline void plan_release(const PlanArgs& a, int b, int lane) {
   }
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
 }
-// One wave: the missing entries of sequence b pop their pages.
-__device__ inline void plan_take(const PlanArgs& a, int b, int lane) {
+// One wave: the missing entries of sequence b pop their pages, from place `at` on downwards.
+__device__ inline void plan_take(const PlanArgs& a, int b, int lane, int at) {
   const PlanRow r = plan_row(a, b);
-  const int first = a.need[b];
-  if (!r.ok || first < 0) return;
-  int at = a.hdr[1] - 1 - first;
   bool bad = false;
   for (int p0 = 0; p0 < r.hi; p0 += 64) {                 // (no needed entry behind hi: n_head <= hi)
     const int p = p0 + lane;
@@ -135,26 +117,93 @@ __device__ inline void plan_take(const PlanArgs& a, int b, int lane) {
     at -= __popcll(m);
   }
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
-  // the last granted sequence's end is the new top
-  if (lane == 0) atomicMin(a.n_free, at + 1);
 }
 
+// Small batches, one launch: a workgroup counts, sums, pushes and pops, a barrier between (its waves take a sequence each; what they
+// write for each other goes through the L1 that they share).  The launches below cost 3 us each, this one 5 to 8 (see plan_one).
+constexpr int PLAN_ONE_MAX = 256;
+static bool plan_one(int B, int max_pages) { return B <= PLAN_ONE_MAX && B * ((max_pages + 63) / 64) <= 256; }
+__global__ __launch_bounds__(1024) void k_plan_one(const PlanArgs a) {
+  __shared__ int32_t s_rel[PLAN_ONE_MAX], s_need[PLAN_ONE_MAX], s_push[PLAN_ONE_MAX], s_pop[PLAN_ONE_MAX];
+  __shared__ int64_t sm[16];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  PlanArgs l = a;
+  l.rel = s_rel;
+  l.need = s_need;
+  for (int b = w; b < a.B; b += 16) plan_count(l, b, lane);
+  const int nf = plan_free(a, tid == 0);
+  __syncthreads();
+  int64_t rel_sum, need_sum;
+  const int need = tid < a.B ? s_need[tid] : 0;
+  const int64_t r = block_scan<1024>((int64_t)(tid < a.B ? plan_given(s_rel[tid]) : 0), tid, sm, rel_sum);
+  const int64_t n = block_scan<1024>((int64_t)max(need, 0), tid, sm, need_sum);
+  const int top = plan_top(a, nf, rel_sum, tid == 0);
+  const int at = plan_grant(need, n, top);
+  if (tid < a.B) {
+    s_push[tid] = (int32_t)min((int64_t)a.n_pages, nf + r);
+    s_pop[tid] = need > 0 ? at : -1;
+    if (a.granted) a.granted[tid] = at >= 0 ? 1 : 0;
+  }
+  // what is left: below the last granted sequence's pages
+  int64_t low = tid < a.B && at >= 0 && need > 0 ? top - (n + need) : top;
+  for (int o = 32; o > 0; o >>= 1) low = min(low, (int64_t)__shfl_xor(low, o, 64));
+  __syncthreads();
+  if (lane == 0) sm[w] = low;
+  for (int b = w; b < a.B; b += 16)
+    if (s_rel[b] != 0) plan_release(l, b, lane, s_push[b]);
+  __syncthreads();
+  for (int b = w; b < a.B; b += 16)
+    if (s_pop[b] >= 0) plan_take(l, b, lane, top - 1 - s_pop[b]);
+  if (tid == 0) {
+    for (int i = 0; i < 16; ++i) low = min(low, sm[i]);
+    a.n_free[0] = (int32_t)low;
+  }
+}
+
+// Large batches.  Every workgroup adds up by itself what the sequences before its four give back (miss).
 __global__ __launch_bounds__(256) void k_plan_count(const PlanArgs a) {
   const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.hdr[0] = plan_free(a, true);
   if (b < a.B) plan_count(a, b, threadIdx.x & 63);
 }
-__global__ __launch_bounds__(1024) void k_plan_scan(const PlanArgs a) {
-  plan_scan(a, threadIdx.x);
-  __syncthreads();
-  if (threadIdx.x == 0) a.n_free[0] = a.hdr[1];           // plan_take lowers it to what is left
+template <typename F>
+__device__ inline int64_t plan_sum(F v, int b0, int B, int64_t* sm, int64_t& total) {
+  int64_t x = 0, y = 0, before;
+  for (int i = threadIdx.x; i < B; i += 256) {
+    const int n = v(i);
+    y += n;
+    x += i < b0 ? n : 0;
+  }
+  block_scan<256>(x, threadIdx.x, sm, before);
+  block_scan<256>(y, threadIdx.x, sm, total);
+  return before;
 }
 __global__ __launch_bounds__(256) void k_plan_release(const PlanArgs a) {
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (b < a.B) plan_release(a, b, threadIdx.x & 63);
+  __shared__ int64_t sm[4];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, b0 = blockIdx.x * 4, b = b0 + w;
+  const int nf = a.hdr[0];
+  int64_t total;
+  auto given = [&](int i) { return plan_given(a.rel[i]); };
+  int64_t before = plan_sum(given, b0, a.B, sm, total);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.n_free[0] = a.hdr[1] = plan_top(a, nf, total, true);   // plan_take lowers it to what is left
+  if (b >= a.B || a.rel[b] == 0) return;
+  for (int i = b0; i < b; ++i) before += given(i);
+  plan_release(a, b, lane, (int)min((int64_t)a.n_pages, nf + before));
 }
 __global__ __launch_bounds__(256) void k_plan_take(const PlanArgs a) {
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (b < a.B) plan_take(a, b, threadIdx.x & 63);
+  __shared__ int64_t sm[4];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, b0 = blockIdx.x * 4, b = b0 + w;
+  const int top = a.hdr[1];
+  int64_t total;
+  auto missing = [&](int i) { return max(a.need[i], 0); };
+  int64_t before = plan_sum(missing, b0, a.B, sm, total);
+  if (b >= a.B) return;
+  for (int i = b0; i < b; ++i) before += missing(i);
+  const int need = a.need[b], at = plan_grant(need, before, top);
+  if (lane == 0 && a.granted) a.granted[b] = at >= 0 ? 1 : 0;
+  if (at < 0 || need == 0) return;
+  if (lane == 0) atomicMin(a.n_free, (int32_t)(top - before - need));
+  plan_take(a, b, lane, top - 1 - at);
 }
 
 hipError_t launch_plan_pages(dllm_ctx* c, hipStream_t s, int n_pages, int B, int keep_head, const int32_t* length, const int32_t* first,
@@ -166,9 +215,12 @@ hipError_t launch_plan_pages(dllm_ctx* c, hipStream_t s, int n_pages, int B, int
   a.hdr = WSC(c, plan, int32_t);
   a.rel = a.hdr + 4;
   a.need = a.rel + c->cfg.max_batch;
+  if (plan_one(B, a.max_pages)) {
+    k_plan_one<<<1, 1024, 0, s>>>(a);
+    return hipGetLastError();
+  }
   const int wgs = (B + 3) / 4;
   k_plan_count<<<wgs, 256, 0, s>>>(a);
-  k_plan_scan<<<1, 1024, 0, s>>>(a);
   k_plan_release<<<wgs, 256, 0, s>>>(a);
   k_plan_take<<<wgs, 256, 0, s>>>(a);
   return hipGetLastError();
@@ -190,58 +242,101 @@ __device__ inline void slot_range(const SlotArgs& a, int b, int& lo, int& hi, bo
   bad = lo != s || hi != e;
   if (hi < lo) hi = lo;
 }
+// Where the sequences' positions start in the list, by one workgroup: for more sequences than k_slot_map adds up by itself.
 __global__ __launch_bounds__(1024) void k_slot_scan(const SlotArgs a) {
-  __shared__ int32_t w_n[16];
-  __shared__ int32_t s_n;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  if (tid == 0) s_n = 0;
-  __syncthreads();
+  __shared__ int32_t sm[16];
+  const int tid = threadIdx.x;
   bool bad = false;
+  int32_t at = 0;
   for (int b0 = 0; b0 < a.B; b0 += 1024) {
     const int b = b0 + tid;
-    int v = 0;
-    if (b < a.B) {
-      int lo, hi;
-      bool x;
-      slot_range(a, b, lo, hi, x);
-      bad |= x;
-      v = hi - lo;
-    }
-    int x = v;
-    for (int o = 1; o < 64; o <<= 1) { const int y = __shfl_up(x, o, 64); if (lane >= o) x += y; }
-    if (lane == 63) w_n[w] = x;
-    __syncthreads();
-    int before = s_n;
-    for (int i = 0; i < w; ++i) before += w_n[i];
-    if (b < a.B) a.cu[b] = before + x - v;
-    __syncthreads();
-    if (tid == 1023) s_n = before + x;
-    __syncthreads();
+    int lo = 0, hi = 0;
+    bool x = false;
+    if (b < a.B) slot_range(a, b, lo, hi, x);
+    bad |= x;
+    int32_t total;
+    const int32_t before = block_scan<1024>(hi - lo, tid, sm, total);
+    if (b < a.B) a.cu[b] = at + before;
+    at += total;
   }
   if (tid == 0) {
-    a.cu[a.B] = s_n;
-    if (s_n > a.capacity) bad = true;
+    a.cu[a.B] = at;
+    if (at > a.capacity) bad = true;
   }
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
 }
-__global__ __launch_bounds__(256) void k_slot_fill(const SlotArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= a.capacity) return;
-  int32_t out = -1;
-  if (i < a.cu[a.B]) {
-    int lo = 0, hi = a.B;                                  // the last sequence that starts at or before i
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.cu[mid] <= i) lo = mid; else hi = mid;
+// A workgroup fills 2048 entries, 4 a thread and pass; up to SLOT_ONE sequences it also adds their lengths up (into LDS; workgroup 0
+// writes cu), so that the call is one launch.
+constexpr int SLOT_ONE = 4096, SLOT_WG = 2048;
+__global__ __launch_bounds__(256) void k_slot_map(const SlotArgs a, int own_scan, int wide) {
+  __shared__ int32_t s_cu[SLOT_ONE + 1], sm[4];
+  const int tid = threadIdx.x;
+  if (own_scan) {
+    const int per = (a.B + 255) / 256;
+    bool bad = false;
+    int32_t sum = 0, total;
+    for (int i = 0; i < per; ++i) {
+      const int b = tid * per + i;
+      int lo, hi;
+      bool x;
+      if (b < a.B) { slot_range(a, b, lo, hi, x); bad |= x; sum += hi - lo; s_cu[b] = hi - lo; }
     }
-    int p0, p1;
-    bool bad;
-    slot_range(a, lo, p0, p1, bad);
-    const int pos = p0 + (int)(i - a.cu[lo]), pi = pos / a.pt;
-    const int page = a.table[(int64_t)lo * a.max_pages + pi];
-    if (page >= 0 && page < a.n_pages) out = page * a.pt + (pos - pi * a.pt);
+    int32_t at = block_scan<256>(sum, tid, sm, total);
+    for (int i = 0; i < per; ++i) {
+      const int b = tid * per + i;
+      if (b < a.B) {
+        const int n = s_cu[b];
+        s_cu[b] = at;
+        if (blockIdx.x == 0) a.cu[b] = at;
+        at += n;
+      }
+    }
+    if (tid == 0) {
+      s_cu[a.B] = total;
+      if (blockIdx.x == 0) { a.cu[a.B] = total; if (total > a.capacity) bad = true; }
+    }
+    if (bad && blockIdx.x == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+    __syncthreads();
   }
-  a.slots[i] = out;
+  const int32_t* const cu = own_scan ? s_cu : a.cu;
+  const int n = cu[a.B];
+  for (int pass = 0; pass < SLOT_WG / 1024; ++pass) {
+    const int64_t i0 = (int64_t)blockIdx.x * SLOT_WG + pass * 1024 + tid * 4;
+    if (i0 >= a.capacity) return;
+    int4 out = make_int4(-1, -1, -1, -1);
+    if (i0 < n) {
+      int b = 0, end = a.B;                                // the last sequence that starts at or before i0
+      while (end - b > 1) {
+        const int mid = (b + end) >> 1;
+        if (cu[mid] <= i0) b = mid; else end = mid;
+      }
+      int first = cu[b], lo = a.start[b], page = -1, pi = -1;
+      lo = (int)min((int64_t)max(lo, 0), (int64_t)a.max_pages * a.pt);
+      int32_t o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t i = i0 + e;
+        o[e] = -1;
+        if (i < n) {
+          while (cu[b + 1] <= i) {
+            ++b;
+            first = cu[b];
+            lo = (int)min((int64_t)max(a.start[b], 0), (int64_t)a.max_pages * a.pt);
+            pi = -1;
+          }
+          const int pos = lo + (int)(i - first), p = pos / a.pt;
+          if (p != pi) { page = a.table[(int64_t)b * a.max_pages + p]; pi = p; }
+          if (page >= 0 && page < a.n_pages) o[e] = page * a.pt + (pos - p * a.pt);
+        }
+      }
+      out = make_int4(o[0], o[1], o[2], o[3]);
+    }
+    if (wide && i0 + 4 <= a.capacity) *(int4*)(a.slots + i0) = out;
+    else {
+      const int32_t o[4] = {out.x, out.y, out.z, out.w};
+      for (int e = 0; e < 4; ++e) if (i0 + e < a.capacity) a.slots[i0 + e] = o[e];
+    }
+  }
 }
 
 hipError_t launch_slot_map(dllm_ctx* c, hipStream_t s, int n_pages, int B, int capacity, const int32_t* start, const int32_t* end,
@@ -250,14 +345,17 @@ hipError_t launch_slot_map(dllm_ctx* c, hipStream_t s, int n_pages, int B, int c
   a.B = B; a.max_pages = c->cfg.max_pages_per_seq; a.pt = c->cfg.page_tokens; a.n_pages = n_pages; a.capacity = capacity;
   a.start = start; a.end = end; a.table = table; a.cu = cu; a.slots = slots;
   a.status = WSC(c, status, int32_t);
-  k_slot_scan<<<1, 1024, 0, s>>>(a);
-  k_slot_fill<<<(unsigned)(((int64_t)capacity + 255) / 256), 256, 0, s>>>(a);
+  const int own_scan = B <= SLOT_ONE;
+  if (!own_scan) k_slot_scan<<<1, 1024, 0, s>>>(a);
+  k_slot_map<<<(unsigned)(((int64_t)capacity + SLOT_WG - 1) / SLOT_WG), 256, 0, s>>>(a, own_scan, ((uintptr_t)slots & 15) == 0);
   return hipGetLastError();
 }
 
 // ==========================================================================================
-// The cache in 4 bits.  One workgroup moves 32 positions of one kv head of one layer: a thread per 32 values that share a scale
-// (one key's 32 channels, one channel's 32 positions), head_dim threads of each kind.
+// The cache in 4 bits.  One workgroup moves 32 positions of one kv head of one layer: 2 * head_dim units of 32 values that share a
+// scale (one key's 32 channels, one channel's 32 positions), four lanes a unit with 8 values (16 bytes of bfloat16, 4 of codes) each, so
+// that neighbouring lanes touch neighbouring bytes on both sides.  Bound: HBM, 4 bytes a value pair of K and V on one side and 1.06 on
+// the other.
 struct Kv4Args {
   int n_tokens, pt, n_pages, n_pages4, hkv;
   char* kv;              // the pool of dllm_create
@@ -266,159 +364,184 @@ struct Kv4Args {
   const int32_t *src, *dst;
   int32_t* status;
 };
+// byte of a record: scale of the 32 channels cb of a key, of a channel
+template <int DH> __device__ __forceinline__ int kv4_k_scale(int key, int cb) {
+  return 32 * DH + ((((key >> 4) << 2) + (key & 3)) * (DH / 32) + cb) * 4 + ((key >> 2) & 3);
+}
+template <int DH> __device__ __forceinline__ int kv4_v_scale(int ch) { return 33 * DH + (ch & 15) * (DH / 16) + (ch >> 4); }
 
 // 2^(byte - 127), byte in 1 .. 254
 __device__ __forceinline__ float pow2_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// 32 bfloat16 values -> 16 bytes of codes and the scale byte
-__device__ inline uint4 kv4_quantise(const bf16_t (&x)[32], uint32_t& byte, bool& odd) {
+// a lane's 8 of a unit's 32 bfloat16 values -> their codes and the unit's scale byte
+__device__ __forceinline__ uint32_t kv4_quantise(const uint32_t (&x)[4], uint32_t& byte, bool& odd) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const uint32_t m = x[i] & 0x7fffu;
-    if (m >= 0x7f80u) odd = true;
-    else top = m > top ? m : top;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = x[i] & 0x7fffu, hi = (x[i] >> 16) & 0x7fffu;
+    odd |= lo >= 0x7f80u || hi >= 0x7f80u;
+    top = max(top, max(lo >= 0x7f80u ? 0u : lo, hi >= 0x7f80u ? 0u : hi));
   }
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
   // max = (1 + m/128) 2^(e-127): 7 * 2^(e-129) holds it up to m = 96, twice that always does
   const int e = (int)(top >> 7) - 2 + ((top & 127u) > 96u ? 1 : 0);
   byte = (uint32_t)(e < 7 ? 7 : (e > 252 ? 252 : e));   // (6 * 2^125 is still a number)
   const float s = pow2_of(byte);
-  uint32_t w[4] = {0, 0, 0, 0};
+  float f[8];
 #pragma unroll
-  for (int i = 0; i < 32; i += 8) {
-    float f[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t b = x[i + j], m = b & 0x7fffu;
-      f[j] = bf16_to_f32((bf16_t)(m > 0x7f80u ? 0u : b));                   // NaN -> 0
-      if (m == 0x7f80u) f[j] = b & 0x8000u ? -6.f * s : 6.f * s;            // infinity: the largest value
-    }
-    // round to nearest, ties to the even code, values beyond 6 become 6
-    uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, f[0], f[1], s, 0);
-    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[2], f[3], s, 1);
-    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[4], f[5], s, 2);
-    v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[6], f[7], s, 3);
-    w[i >> 3] = v;
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t b = x[i >> 1] << (i & 1 ? 0 : 16) & 0xffff0000u, m = b & 0x7fffffffu;
+    f[i] = __uint_as_float(m > 0x7f800000u ? 0u : b);                       // NaN -> 0
+    if (m == 0x7f800000u) f[i] = b >> 31 ? -6.f * s : 6.f * s;              // infinity: the largest value
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  // round to nearest, ties to the even code, values beyond 6 become 6
+  uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, f[0], f[1], s, 0);
+  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[2], f[3], s, 1);
+  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[4], f[5], s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[6], f[7], s, 3);
+}
+// the values of 8 codes under a scale, as bfloat16 (exact)
+__device__ __forceinline__ uint4 kv4_values(uint32_t codes, uint32_t byte) {
+  const float s = pow2_of(byte);
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3)));
+}
+// The 32 lanes' slots are one behind the other in a page, the first a multiple of 8 (asked by both halves of a wave): V of a
+// channel is then 16-byte pieces.
+__device__ __forceinline__ bool slots_run(int s, int i, int pt) {
+  const int s0 = __shfl(s, 0, 64);
+  return s0 >= 0 && __builtin_amdgcn_ballot_w64(!(s == s0 + i && s0 % pt + i < pt)) == 0 && s0 % 8 == 0;
 }
 
 template <int DH>
-__global__ __launch_bounds__(2 * DH) void k_kv4_store(const Kv4Args a) {
+__global__ __launch_bounds__(256) void k_kv4_store(const Kv4Args a) {
+  constexpr int NG = DH / 32, IT = DH / 32;               // 16-byte pieces of K, of V: 4 * DH each
   __shared__ int32_t s_src[32];
-  __shared__ int s_ok, s_run;
+  __shared__ int s_ok, s_run, s_dst;
   const int tid = threadIdx.x, grp = blockIdx.x, h = blockIdx.y, layer = blockIdx.z;
   const int n_slots = a.n_pages * a.pt, n_slots4 = a.n_pages4 * a.pt;       // (below 2^31, checked by the call)
   if (tid < 64) {
     const int i = tid & 31;
-    const int d0 = a.dst[(int64_t)grp * 32], d = a.dst[(int64_t)grp * 32 + i], s = a.src[(int64_t)grp * 32 + i];
+    const int d = a.dst[(int64_t)grp * 32 + i], s = a.src[(int64_t)grp * 32 + i], d0 = __shfl(d, 0, 64);
     const bool none = __builtin_amdgcn_ballot_w64(d != -1) == 0;
     const bool good = d0 >= 0 && d0 < n_slots4 && (d0 & 31) == 0 && d == d0 + i && s >= 0 && s < n_slots;
-    const bool all = __builtin_amdgcn_ballot_w64(!good) == 0;
-    // the 32 positions one behind the other in a page, from a multiple of 8 on: 16-byte reads of V
-    const int s0 = a.src[(int64_t)grp * 32];
-    const bool run = __builtin_amdgcn_ballot_w64(!(s == s0 + i && s0 % a.pt + i < a.pt)) == 0 && s0 % 8 == 0 && a.pt % 8 == 0;
+    const bool all = __builtin_amdgcn_ballot_w64(!good) == 0, run = slots_run(s, i, a.pt);
     if (tid < 32) s_src[i] = s;
     if (tid == 0) {
       s_ok = all;
       s_run = run;
+      s_dst = d0;
       if (!all && !none && h == 0 && layer == 0) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
     }
   }
   __syncthreads();
   if (!s_ok) return;
-  const int d0 = a.dst[(int64_t)grp * 32], page4 = d0 / a.pt, g4 = (d0 - page4 * a.pt) >> 5;
-  const int64_t rec_at = (((int64_t)layer * a.n_pages4 + page4) * a.hkv + h) * (a.pt >> 5) + g4;
-  uint8_t* const rec = a.kv4 + rec_at * 34 * DH;
-  bf16_t x[32];
-  if (tid < DH) {                                           // one key's 32 channels
-    constexpr int NG = DH / 32;
-    const int key = tid / NG, cb = tid % NG, s = s_src[key], page = s / a.pt;
-    const bf16_t* p = (const bf16_t*)a.kv + (2 * layer) * a.slab + (((int64_t)page * a.hkv + h) * a.pt + (s - page * a.pt)) * DH + cb * 32;
+  const int d0 = s_dst, page4 = d0 / a.pt, g4 = (d0 - page4 * a.pt) >> 5;
+  uint8_t* const rec = a.kv4 + ((((int64_t)layer * a.n_pages4 + page4) * a.hkv + h) * (a.pt >> 5) + g4) * 34 * DH;
+  const bf16_t* const ks = (const bf16_t*)a.kv + (2 * (int64_t)layer) * a.slab;
+  const bf16_t* const vs = ks + a.slab;
+  bool odd = false;
+  uint32_t x[IT][4], byte;
+  const bool run = s_run;
+  const int s0 = s_src[0], page0 = s0 / a.pt;
+  const int64_t ph0 = (int64_t)page0 * a.hkv + h;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *(uint4*)(x + 8 * i) = *(const uint4*)(p + 8 * i);
-    uint32_t byte;
-    bool odd = false;
-    const uint4 w = kv4_quantise(x, byte, odd);
-    *(uint4*)(rec + key * (DH / 2) + cb * 16) = w;
-    rec[32 * DH + ((((key >> 4) << 2) + (key & 3)) * NG + cb) * 4 + ((key >> 2) & 3)] = (uint8_t)byte;
-    if (odd) atomicOr(a.status, DLLM_STATUS_NOT_FINITE);
-  } else {                                                  // one channel's 32 positions
-    const int ch = tid - DH;
-    const bf16_t* slab = (const bf16_t*)a.kv + (2 * layer + 1) * a.slab;
-    if (s_run) {
-      const int s = s_src[0], page = s / a.pt;
-      const bf16_t* p = slab + (((int64_t)page * a.hkv + h) * DH + ch) * a.pt + (s - page * a.pt);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) *(uint4*)(x + 8 * i) = *(const uint4*)(p + 8 * i);
+  for (int it = 0; it < IT; ++it) {                       // IT / 2 rounds of K (DH 64: one), then of V
+    const int item = it * 256 + tid, u = item >> 2, part = item & 3;
+    if (u < DH) {
+      const int key = u / NG, cb = u % NG, s = s_src[key], page = s / a.pt;
+      *(uint4*)x[it] = *(const uint4*)(ks + (((int64_t)page * a.hkv + h) * a.pt + (s - page * a.pt)) * DH + cb * 32 + part * 8);
+    } else if (run) {
+      *(uint4*)x[it] = *(const uint4*)(vs + (ph0 * DH + (u - DH)) * a.pt + (s0 - page0 * a.pt) + part * 8);
     } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const int s = s_src[i], page = s / a.pt;
-        x[i] = slab[(((int64_t)page * a.hkv + h) * DH + ch) * a.pt + (s - page * a.pt)];
+      for (int e = 0; e < 8; ++e) {
+        const int s = s_src[part * 8 + e], page = s / a.pt;
+        const uint32_t v = vs[(((int64_t)page * a.hkv + h) * DH + (u - DH)) * a.pt + (s - page * a.pt)];
+        x[it][e >> 1] = e & 1 ? x[it][e >> 1] | v << 16 : v;
       }
     }
-    uint32_t byte;
-    bool odd = false;
-    const uint4 w = kv4_quantise(x, byte, odd);
-    *(uint4*)(rec + 16 * DH + ch * 16) = w;
-    rec[33 * DH + (ch & 15) * (DH / 16) + (ch >> 4)] = (uint8_t)byte;
-    if (odd) atomicOr(a.status, DLLM_STATUS_NOT_FINITE);
   }
-}
-
-// the value of a code under a scale, as bfloat16 (exact)
-__device__ __forceinline__ bf16_t kv4_value(uint32_t code, uint32_t byte) {
-  // 0, 1/2, 1, 3/2, 2, 3, 4, 6 in eighths of their binade: (code & 1) is the mantissa bit, codes 0 and 1 have none
-  const uint32_t m = code & 7u;
-  const float f = (float)(m < 2 ? m : (2u + (m & 1u)) << ((m >> 1) - 1)) * 0.5f * pow2_of(byte);
-  return f32_to_bf16(code & 8u ? -f : f);
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int item = it * 256 + tid, u = item >> 2, part = item & 3;
+    const uint32_t w = kv4_quantise(x[it], byte, odd);
+    *(uint32_t*)(rec + u * 16 + part * 4) = w;            // (K and V codes: 16 bytes a unit, one behind the other)
+    if (part == 0) rec[u < DH ? kv4_k_scale<DH>(u / NG, u % NG) : kv4_v_scale<DH>(u - DH)] = (uint8_t)byte;
+  }
+  if (odd) atomicOr(a.status, DLLM_STATUS_NOT_FINITE);
 }
 
 template <int DH>
-__global__ __launch_bounds__(2 * DH) void k_kv4_load(const Kv4Args a) {
-  constexpr int NG = DH / 32;
+__global__ __launch_bounds__(256) void k_kv4_load(const Kv4Args a) {
+  constexpr int NG = DH / 32, IT = DH / 32;
   __shared__ int32_t s_src[32], s_dst[32];
+  __shared__ int s_run;
   const int tid = threadIdx.x, h = blockIdx.y, layer = blockIdx.z;
   const int64_t i0 = (int64_t)blockIdx.x * 32;
   const int n_slots = a.n_pages * a.pt, n_slots4 = a.n_pages4 * a.pt;
-  if (tid < 32) {
+  if (tid < 64) {
+    const int i = tid & 31;
     int s = -1, d = -1;
-    if (i0 + tid < a.n_tokens) { s = a.src[i0 + tid]; d = a.dst[i0 + tid]; }
+    if (i0 + i < a.n_tokens) { s = a.src[i0 + i]; d = a.dst[i0 + i]; }
     const bool ok = s >= 0 && s < n_slots4 && d >= 0 && d < n_slots;
+    const bool all = __builtin_amdgcn_ballot_w64(!ok) == 0;
+    const bool run = slots_run(s, i, a.pt) && slots_run(d, i, a.pt) && (__shfl(s, 0, 64) & 31) == 0;   // a whole record to a run
     if (!ok && !(s == -1 && d == -1) && h == 0 && layer == 0) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
-    s_src[tid] = ok ? s : -1;
-    s_dst[tid] = d;
+    if (tid < 32) { s_src[i] = ok ? s : -1; s_dst[i] = d; }
+    if (tid == 0) s_run = all && run;
   }
   __syncthreads();
   auto record = [&](int s) -> const uint8_t* {
     const int page = s / a.pt, g = (s - page * a.pt) >> 5;
     return a.kv4 + ((((int64_t)layer * a.n_pages4 + page) * a.hkv + h) * (a.pt >> 5) + g) * 34 * DH;
   };
-  if (tid < DH) {
-    const int i = tid / NG, cb = tid % NG, s = s_src[i];
-    if (s < 0) return;
-    const uint8_t* rec = record(s);
-    const int key = s & 31, d = s_dst[i], page = d / a.pt;
-    const uint4 w = *(const uint4*)(rec + key * (DH / 2) + cb * 16);
-    const uint32_t byte = rec[32 * DH + ((((key >> 4) << 2) + (key & 3)) * NG + cb) * 4 + ((key >> 2) & 3)];
-    bf16_t* p = (bf16_t*)a.kv + (2 * layer) * a.slab + (((int64_t)page * a.hkv + h) * a.pt + (d - page * a.pt)) * DH + cb * 32;
-    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-    bf16_t x[32];
+  bf16_t* const ks = (bf16_t*)a.kv + (2 * (int64_t)layer) * a.slab;
+  bf16_t* const vs = ks + a.slab;
+  auto k_row = [&](int d, int cb, int part) -> bf16_t* {
+    const int page = d / a.pt;
+    return ks + (((int64_t)page * a.hkv + h) * a.pt + (d - page * a.pt)) * DH + cb * 32 + part * 8;
+  };
+  auto v_at = [&](int d, int ch) -> bf16_t* {
+    const int page = d / a.pt;
+    return vs + (((int64_t)page * a.hkv + h) * DH + ch) * a.pt + (d - page * a.pt);
+  };
+  if (s_run) {
+    const uint8_t* const rec = record(s_src[0]);
+    uint32_t w[IT], byte[IT];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) x[e] = kv4_value(ww[e >> 3] >> (4 * (e & 7)) & 15u, byte);
+    for (int it = 0; it < IT; ++it) {
+      const int item = it * 256 + tid, u = item >> 2, part = item & 3;
+      w[it] = *(const uint32_t*)(rec + u * 16 + part * 4);
+      byte[it] = rec[u < DH ? kv4_k_scale<DH>(u / NG, u % NG) : kv4_v_scale<DH>(u - DH)];
+    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) *(uint4*)(p + 8 * e) = *(const uint4*)(x + 8 * e);
-  } else {
-    const int ch = tid - DH;
-    bf16_t* slab = (bf16_t*)a.kv + (2 * layer + 1) * a.slab;
-    for (int i = 0; i < 32; ++i) {
-      const int s = s_src[i];
+    for (int it = 0; it < IT; ++it) {
+      const int item = it * 256 + tid, u = item >> 2, part = item & 3;
+      *(uint4*)(u < DH ? k_row(s_dst[u / NG], u % NG, part) : v_at(s_dst[0], u - DH) + part * 8) = kv4_values(w[it], byte[it]);
+    }
+    return;
+  }
+  for (int it = 0; it < IT; ++it) {
+    const int item = it * 256 + tid, u = item >> 2, part = item & 3;
+    if (u < DH) {
+      const int i = u / NG, cb = u % NG, s = s_src[i];
       if (s < 0) continue;
       const uint8_t* rec = record(s);
-      const int d = s_dst[i], page = d / a.pt;
-      const uint32_t code = rec[16 * DH + ch * 16 + ((s & 31) >> 1)] >> (4 * (s & 1)) & 15u;
-      slab[(((int64_t)page * a.hkv + h) * DH + ch) * a.pt + (d - page * a.pt)] = kv4_value(code, rec[33 * DH + (ch & 15) * (DH / 16) + (ch >> 4)]);
+      const int key = s & 31;
+      *(uint4*)k_row(s_dst[i], cb, part) = kv4_values(*(const uint32_t*)(rec + (key * NG + cb) * 16 + part * 4), rec[kv4_k_scale<DH>(key, cb)]);
+    } else {
+      const int ch = u - DH;
+      for (int e = 0; e < 8; ++e) {
+        const int s = s_src[part * 8 + e];
+        if (s < 0) continue;
+        const uint8_t* rec = record(s);
+        const uint32_t code = rec[16 * DH + ch * 16 + ((s & 31) >> 1)] >> (4 * (s & 1)) & 15u;
+        *v_at(s_dst[part * 8 + e], ch) = (bf16_t)kv4_values(code, rec[kv4_v_scale<DH>(ch)]).x;
+      }
     }
   }
 }
@@ -438,7 +561,7 @@ hipError_t launch_kv4_store(dllm_ctx* c, hipStream_t s, int n_tokens, const int3
   const Kv4Args a = kv4_args(c, n_tokens, src, dst);
   const dim3 grid(n_tokens / 32, c->cfg.n_kv_heads, c->cfg.n_layers);
   if (c->cfg.head_dim == 128) k_kv4_store<128><<<grid, 256, 0, s>>>(a);
-  else k_kv4_store<64><<<grid, 128, 0, s>>>(a);
+  else k_kv4_store<64><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -447,7 +570,7 @@ hipError_t launch_kv4_load(dllm_ctx* c, hipStream_t s, int n_tokens, const int32
   const Kv4Args a = kv4_args(c, n_tokens, src, dst);
   const dim3 grid((n_tokens + 31) / 32, c->cfg.n_kv_heads, c->cfg.n_layers);
   if (c->cfg.head_dim == 128) k_kv4_load<128><<<grid, 256, 0, s>>>(a);
-  else k_kv4_load<64><<<grid, 128, 0, s>>>(a);
+  else k_kv4_load<64><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
