@@ -27,6 +27,17 @@ __device__ inline PlanRow plan_row(const PlanArgs& a, int b) {
 }
 __device__ inline bool plan_needed(const PlanRow& r, int p) { return p < r.n_head || (p >= r.lo && p < r.hi); }
 
+// Entries p0 .. p0 + PLAN_ROW - 1 of a row, requested together (-1 from `end` on): the walks below would wait for each 64 otherwise.
+constexpr int PLAN_ROW = 512;
+__device__ inline void plan_row_entries(const PlanArgs& a, int b, int p0, int lane, int end, int32_t (&e)[PLAN_ROW / 64]) {
+  const int32_t* const row = a.table + (int64_t)b * a.max_pages;
+#pragma unroll
+  for (int i = 0; i < PLAN_ROW / 64; ++i) {
+    const int p = p0 + i * 64 + lane;
+    e[i] = row[min(p, a.max_pages - 1)];
+    if (p >= end) e[i] = -1;
+  }
+}
 __device__ inline int plan_given(int rel) { return rel < 0 ? ~rel : rel; }
 
 // One wave: pages that sequence b gives back and entries it misses.
@@ -34,12 +45,18 @@ __device__ inline void plan_count(const PlanArgs& a, int b, int lane) {
   const PlanRow r = plan_row(a, b);
   int rel = 0, need = 0;
   bool wrong = false;
-  for (int p = lane; p < a.max_pages && r.ok; p += 64) {
-    const int e = a.table[(int64_t)b * a.max_pages + p];
-    const bool n = plan_needed(r, p);
-    rel += e >= 0 && e < a.n_pages && !n;
-    wrong |= e >= a.n_pages && !n;
-    need += e < 0 && n;
+  for (int p0 = 0; p0 < a.max_pages && r.ok; p0 += PLAN_ROW) {
+    int32_t e[PLAN_ROW / 64];
+    plan_row_entries(a, b, p0, lane, a.max_pages, e);
+#pragma unroll
+    for (int i = 0; i < PLAN_ROW / 64; ++i) {
+      const int p = p0 + i * 64 + lane;
+      if (p0 + i * 64 >= a.max_pages) break;
+      const bool in = p < a.max_pages, n = plan_needed(r, p);
+      rel += in && e[i] >= 0 && e[i] < a.n_pages && !n;
+      wrong |= in && e[i] >= a.n_pages && !n;
+      need += in && e[i] < 0 && n;
+    }
   }
   for (int o = 32; o > 0; o >>= 1) { rel += __shfl_xor(rel, o, 64); need += __shfl_xor(need, o, 64); }
   const bool any = __builtin_amdgcn_ballot_w64(wrong) != 0;
@@ -85,17 +102,21 @@ __device__ inline void plan_release(const PlanArgs& a, int b, int lane, int at) 
   const PlanRow r = plan_row(a, b);
   if (!r.ok) return;
   bool bad = false;
-  for (int p0 = 0; p0 < a.max_pages; p0 += 64) {
-    const int p = p0 + lane;
-    int32_t* const e = a.table + (int64_t)b * a.max_pages + p;
-    const int v = p < a.max_pages ? *e : -1;
-    const bool gone = v >= 0 && !plan_needed(r, p), push = gone && v < a.n_pages;
-    const uint64_t m = __builtin_amdgcn_ballot_w64(push);
-    const int slot = at + __popcll(m & ((1ull << lane) - 1));
-    if (push && slot < a.n_pages) a.stack[slot] = v;
-    if (gone) *e = -1;
-    bad |= gone && !push;
-    at += __popcll(m);
+  for (int p0 = 0; p0 < a.max_pages; p0 += PLAN_ROW) {
+    int32_t e[PLAN_ROW / 64];
+    plan_row_entries(a, b, p0, lane, a.max_pages, e);
+#pragma unroll
+    for (int i = 0; i < PLAN_ROW / 64; ++i) {
+      const int p = p0 + i * 64 + lane;
+      if (p0 + i * 64 >= a.max_pages) break;
+      const bool gone = e[i] >= 0 && !plan_needed(r, p), push = gone && e[i] < a.n_pages;
+      const uint64_t m = __builtin_amdgcn_ballot_w64(push);
+      const int slot = at + __popcll(m & ((1ull << lane) - 1));
+      if (push && slot < a.n_pages) a.stack[slot] = e[i];
+      if (gone) a.table[(int64_t)b * a.max_pages + p] = -1;
+      bad |= gone && !push;
+      at += __popcll(m);
+    }
   }
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
 }
@@ -103,61 +124,69 @@ __device__ inline void plan_release(const PlanArgs& a, int b, int lane, int at) 
 __device__ inline void plan_take(const PlanArgs& a, int b, int lane, int at) {
   const PlanRow r = plan_row(a, b);
   bool bad = false;
-  for (int p0 = 0; p0 < r.hi; p0 += 64) {                 // (no needed entry behind hi: n_head <= hi)
-    const int p = p0 + lane;
-    int32_t* const e = a.table + (int64_t)b * a.max_pages + p;
-    const bool miss = p < r.hi && plan_needed(r, p) && *e < 0;
-    const uint64_t m = __builtin_amdgcn_ballot_w64(miss);
-    if (miss) {
-      const int page = a.stack[at - __popcll(m & ((1ull << lane) - 1))];
-      const bool ok = page >= 0 && page < a.n_pages;
-      *e = ok ? page : -1;
-      bad |= !ok;
+  for (int p0 = 0; p0 < r.hi; p0 += PLAN_ROW) {           // (no needed entry behind hi: n_head <= hi)
+    int32_t e[PLAN_ROW / 64], page[PLAN_ROW / 64];
+    plan_row_entries(a, b, p0, lane, a.max_pages, e);
+    uint32_t miss = 0;
+#pragma unroll
+    for (int i = 0; i < PLAN_ROW / 64; ++i) {
+      const int p = p0 + i * 64 + lane;
+      page[i] = 0;
+      if (p0 + i * 64 >= r.hi) continue;
+      const bool x = p < r.hi && plan_needed(r, p) && e[i] < 0;
+      const uint64_t m = __builtin_amdgcn_ballot_w64(x);
+      page[i] = x ? a.stack[at - __popcll(m & ((1ull << lane) - 1))] : 0;
+      miss |= (uint32_t)x << i;
+      at -= __popcll(m);
     }
-    at -= __popcll(m);
+#pragma unroll
+    for (int i = 0; i < PLAN_ROW / 64; ++i)
+      if (miss >> i & 1) {
+        const bool ok = page[i] >= 0 && page[i] < a.n_pages;
+        a.table[(int64_t)b * a.max_pages + p0 + i * 64 + lane] = ok ? page[i] : -1;
+        bad |= !ok;
+      }
   }
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
 }
 
-// Small batches, one launch: a workgroup counts, sums, pushes and pops, a barrier between (its waves take a sequence each; what they
-// write for each other goes through the L1 that they share).  The launches below cost 3 us each, this one 5 to 8 (see plan_one).
-constexpr int PLAN_ONE_MAX = 256;
-static bool plan_one(int B, int max_pages) { return B <= PLAN_ONE_MAX && B * ((max_pages + 63) / 64) <= 256; }
+// Small batches, one launch: a workgroup with a wave a sequence counts, sums, pushes and pops, a barrier between (what the waves write
+// for each other goes through the L1 that they share).  us in a graph, this / three launches: 8 rows of 40 entries 3.7 / 7.0, 16 of 64
+// 5.9 / 8.8, 16 of 512 7.6 / 9.2; two rows a wave: 32 of 64 10.2 / 9.3, 32 of 512 16.8 / 10.9.
+constexpr int PLAN_ONE_MAX = 16;
+static bool plan_one(int B, int max_pages) { return B <= PLAN_ONE_MAX && max_pages <= PLAN_ROW; }
 __global__ __launch_bounds__(1024) void k_plan_one(const PlanArgs a) {
   __shared__ int32_t s_rel[PLAN_ONE_MAX], s_need[PLAN_ONE_MAX], s_push[PLAN_ONE_MAX], s_pop[PLAN_ONE_MAX];
-  __shared__ int64_t sm[16];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   PlanArgs l = a;
   l.rel = s_rel;
   l.need = s_need;
-  for (int b = w; b < a.B; b += 16) plan_count(l, b, lane);
-  const int nf = plan_free(a, tid == 0);
+  if (w < a.B) plan_count(l, w, lane);
   __syncthreads();
-  int64_t rel_sum, need_sum;
-  const int need = tid < a.B ? s_need[tid] : 0;
-  const int64_t r = block_scan<1024>((int64_t)(tid < a.B ? plan_given(s_rel[tid]) : 0), tid, sm, rel_sum);
-  const int64_t n = block_scan<1024>((int64_t)max(need, 0), tid, sm, need_sum);
-  const int top = plan_top(a, nf, rel_sum, tid == 0);
-  const int at = plan_grant(need, n, top);
-  if (tid < a.B) {
-    s_push[tid] = (int32_t)min((int64_t)a.n_pages, nf + r);
-    s_pop[tid] = need > 0 ? at : -1;
-    if (a.granted) a.granted[tid] = at >= 0 ? 1 : 0;
+  if (w == 0) {                                            // a lane a sequence
+    const int nf = plan_free(a, lane == 0);
+    const int rel = lane < a.B ? plan_given(s_rel[lane]) : 0, need = lane < a.B ? s_need[lane] : 0;
+    int64_t r = rel, n = max(need, 0);
+    for (int o = 1; o < PLAN_ONE_MAX; o <<= 1) {
+      const int64_t x = __shfl_up(r, o, 64), y = __shfl_up(n, o, 64);
+      if (lane >= o) { r += x; n += y; }
+    }
+    const int top = plan_top(a, nf, __shfl(r, PLAN_ONE_MAX - 1, 64), lane == 0);
+    const int at = plan_grant(need, n - max(need, 0), top);
+    if (lane < a.B) {
+      s_push[lane] = (int32_t)min((int64_t)a.n_pages, nf + r - rel);
+      s_pop[lane] = need > 0 && at >= 0 ? top - 1 - at : -1;
+      if (a.granted) a.granted[lane] = at >= 0 ? 1 : 0;
+    }
+    // what is left: below the last granted sequence's pages
+    int left = (int)(lane < a.B && at >= 0 && need > 0 ? top - n : top);
+    for (int o = 32; o > 0; o >>= 1) left = min(left, __shfl_xor(left, o, 64));
+    if (lane == 0) a.n_free[0] = left;
   }
-  // what is left: below the last granted sequence's pages
-  int64_t low = tid < a.B && at >= 0 && need > 0 ? top - (n + need) : top;
-  for (int o = 32; o > 0; o >>= 1) low = min(low, (int64_t)__shfl_xor(low, o, 64));
   __syncthreads();
-  if (lane == 0) sm[w] = low;
-  for (int b = w; b < a.B; b += 16)
-    if (s_rel[b] != 0) plan_release(l, b, lane, s_push[b]);
+  if (w < a.B && s_rel[w] != 0) plan_release(l, w, lane, s_push[w]);
   __syncthreads();
-  for (int b = w; b < a.B; b += 16)
-    if (s_pop[b] >= 0) plan_take(l, b, lane, top - 1 - s_pop[b]);
-  if (tid == 0) {
-    for (int i = 0; i < 16; ++i) low = min(low, sm[i]);
-    a.n_free[0] = (int32_t)low;
-  }
+  if (w < a.B && s_pop[w] >= 0) plan_take(l, w, lane, s_pop[w]);
 }
 
 // Large batches.  Every workgroup adds up by itself what the sequences before its four give back (miss).
