@@ -11,7 +11,8 @@ struct AttendArgs {
   const void *k, *v;        // slabs of the layer
   const uint8_t* kv4;       // records of the layer
   int B, Q, Hq, Hkv, max_prefix, window, n_sink;
-  int pt, pt_shift, max_pages, n_pages, n_pages4;   // pt_shift: log2(pt) if that is a power of two of at least 32, else -1
+  int pt, max_pages, n_pages, n_pages4;
+  uint32_t pt_inv;          // key / pt = the high word of key * pt_inv (k_attend)
   int32_t* status;
   // k_attend
   int n_rg_wg, kspl;        // row groups of a workgroup, its waves along the keys of each
@@ -162,6 +163,7 @@ __global__ __launch_bounds__(256) void k_attend_any(const AttendArgs a, int dh) 
 // 4t+3 of the second product's operand.  With 64 channels k holds them twice, against hi and lo of the query.
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef const int32_t __attribute__((address_space(4)))* const_i32;   // what a launch only reads, by scalar loads
 
 template <int SEL>
 __device__ __forceinline__ f32x4 mfma4(u32x4 a, i32x8 b, f32x4 c, uint32_t scale_a, uint32_t scale_b) {
@@ -237,21 +239,21 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv;
   const int G = a.Hq / a.Hkv;
   const AttendSeq sq = attend_seq(a, b);
-  if (sq.bad && threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
   const int n_q = sq.n_q, R = n_q * G, kv_len = sq.kv_len, n4 = sq.n4;
-  if (blockIdx.y * a.n_rg_wg * 16 * QT >= R) return;           // (the whole workgroup)
+  if (blockIdx.y * a.n_rg_wg * 16 * QT >= R) {                 // (the whole workgroup)
+    if (sq.bad && threadIdx.x == 0 && blockIdx.y == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+    return;
+  }
   const bool active = rg * 16 * QT < R;
   const int U = a.n_parts * a.kspl, unit = blockIdx.z * a.kspl + kw;
 
   // the lane's queries, and what the wave's rows read: [0, n_head) and [lo, kv_len), all of it from lo_all on
-  int64_t row_out[QT];
   int row_in[QT], wlo[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = rg * 16 * QT + t * 16 + c, rr = min(r, R - 1);
     const int hg = rr / n_q, j = rr - hg * n_q;
     row_in[t] = (b * a.Q + j) * a.Hq + kvh * G + hg;
-    row_out[t] = r < R ? row_in[t] : -1;
     wlo[t] = a.window > 0 ? sq.pl + j - a.window : -1;         // keys above it are read
   }
   int lo = 0, lo_all = 0, n_head = 0;
@@ -262,8 +264,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     lo_all = max(0, sq.pl + (one ? r1 % n_q : n_q - 1) - a.window + 1);
     n_head = min(a.n_sink, lo);
   }
-  auto read_all = [&](int k0, int k1) { return k1 <= a.n_sink || k0 >= lo_all; };     // every row reads keys k0 .. k1 - 1
-  auto read_any = [&](int k0, int k1) { return k0 < n_head || k1 > lo; };             // some row may
+  auto read_all = [&](int k0, int k1) { return (bool)((k1 <= a.n_sink) | (k0 >= lo_all)); };     // every row reads keys k0 .. k1 - 1
+  auto read_any = [&](int k0, int k1) { return (bool)((k0 < n_head) | (k1 > lo)); };             // some row may
 
   f32x4 oacc[DT][QT];
   float m_run[QT], l_run[QT];
@@ -276,15 +278,13 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   }
   bool bad = false;
   const bf16_t* const q = (const bf16_t*)a.q;
-  int n_blk4 = 0;
 
   // ---- keys in 4 bits, blocks of 128: those of the head, then those from lo on
-  if (n4 > 0 && active) {
-    const int first = min(lo, n4) >> 7, last = (n4 + 127) >> 7;
-    const int n_b = lo < n4 ? last - first : 0;
-    int n_a = (min(n_head, n4) + 127) >> 7;
-    if (n_b > 0) n_a = min(n_a, first);
-    n_blk4 = n_a + n_b;
+  const int first = min(lo, n4) >> 7, n_b = lo < n4 ? ((n4 + 127) >> 7) - first : 0;
+  int n_a = (min(n_head, n4) + 127) >> 7;
+  if (n_b > 0) n_a = min(n_a, first);
+  const int n_blk4 = n_a + n_b;
+  if (active && unit < n_blk4) {
     i32x8 qh[QT], ql[DH == 128 ? QT : 1];
     uint32_t qs[QT];                                            // scale bytes: hi, lo in the next byte (DH 64: the lane's own)
 #pragma unroll
@@ -320,138 +320,205 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
       }
     }
     const int gpp = a.pt >> 5;                                  // groups of 32 a page
-    const int32_t* const table = a.table4 + (int64_t)b * a.max_pages;
-    const int gk = (c >> 3), kin = 16 * ((c >> 2) & 1) + (c & 3), gch = DH == 128 ? g : g & 1;
-    const int k_off = kin * (DH / 2) + gch * 16, ks_off = 32 * DH + (((c >> 2) & 1) * 4 + (c & 3)) * (DH / 8) + gch * 4;
+    const const_i32 table = (const_i32)(uintptr_t)(a.table4 + (int64_t)b * a.max_pages);
+    const int gch = DH == 128 ? g : g & 1;
+    const int k_off = (16 * ((c >> 2) & 1) + (c & 3)) * (DH / 2) + gch * 16, ks_off = 32 * DH + (((c >> 2) & 1) * 4 + (c & 3)) * (DH / 8) + gch * 4;
     const int v_off = 16 * DH + c * 16, vs_off = 33 * DH + c * (DH / 16);
-    auto block_at = [&](int i) { return i < n_a ? i : first + (i - n_a); };
-    // records of the groups whose keys (two halves) and values the lane loads: table entries first, a block ahead
-    // (no branch around a load: it would wait for all of them)
-    auto page_of = [&](int grp) { return a.pt_shift >= 0 ? grp >> (a.pt_shift - 5) : grp / gpp; };
-    auto entry = [&](int grp) { const int pi = page_of(grp), e = table[min(pi, a.max_pages - 1)]; return pi < a.max_pages ? e : -1; };
-    auto record = [&](int grp, int page, bool& ok) -> const uint8_t* {
-      ok = (uint32_t)page < (uint32_t)a.n_pages4;
-      return a.kv4 + (((int64_t)(ok ? page : 0) * a.Hkv + kvh) * gpp + (grp - page_of(grp) * gpp)) * (34 * DH);
+    // A block's four records (scalar work): their bases, and which of them hold no key that is read or cannot be addressed - anything
+    // may lie there.  Table entries are asked for a block ahead.
+    struct Ent { int e0, e1, e2, e3; };
+    struct Recs { int64_t k0, k1, v; uint32_t dead; };          // the lane's: K of the first 64 keys, of the others, V
+    auto key_of = [&](int i) { const int j = min(i, n_blk4 - 1); return (j < n_a ? j : first + (j - n_a)) << 7; };
+    auto page_of = [&](int key) { return (int)__umulhi((uint32_t)key, a.pt_inv); };
+    auto entry = [&](int key) { return table[min(page_of(key), a.max_pages - 1)]; };
+    auto entries = [&](int k0) { return Ent{entry(k0), entry(k0 + 32), entry(k0 + 64), entry(k0 + 96)}; };
+    auto record = [&](int key, int page, uint32_t bit, uint32_t& dead) -> int64_t {
+      const int pi = page_of(key);
+      const bool ok = (pi < a.max_pages) & ((uint32_t)page < (uint32_t)a.n_pages4), want = (key < n4) & read_any(key, key + 32);
+      bad |= want & !ok;
+      dead |= want & ok ? 0u : bit;
+      return (((int64_t)(ok ? page : 0) * a.Hkv + kvh) * gpp + ((key - pi * a.pt) >> 5)) * (34 * DH);
     };
-    int e0, e1, ev;
-    {
-      const int g0 = block_at(min(unit, n_blk4 - 1)) << 2;
-      e0 = entry(g0 + gk); e1 = entry(g0 + 2 + gk); ev = entry(g0 + g);
-    }
+    auto records = [&](int k0, const Ent& x) {
+      Recs r;
+      uint32_t dead = 0;
+      const int64_t r0 = record(k0, x.e0, 1, dead), r1 = record(k0 + 32, x.e1, 2, dead), r2 = record(k0 + 64, x.e2, 4, dead),
+                    r3 = record(k0 + 96, x.e3, 8, dead);
+      r.k0 = c & 8 ? r1 : r0;
+      r.k1 = c & 8 ? r3 : r2;
+      const int64_t va = g & 1 ? r1 : r0, vb = g & 1 ? r3 : r2;
+      r.v = g & 2 ? vb : va;
+      r.dead = dead;
+      return r;
+    };
+    u32x4 kf[8], vf[DT];
+    uint32_t ks[2], vs[DT / 4];
+    auto load_k = [&](const Recs& r) {
+      const uint8_t *p0 = a.kv4 + (r.k0 + k_off), *p1 = a.kv4 + (r.k1 + k_off);
+      ks[0] = *(const uint32_t*)(p0 + (ks_off - k_off));
+      ks[1] = *(const uint32_t*)(p1 + (ks_off - k_off));
+#pragma unroll
+      for (int t = 0; t < 8; ++t) kf[t] = *(const u32x4*)((t < 4 ? p0 : p1) + (t & 3) * 4 * (DH / 2));
+    };
+    auto load_v = [&](const Recs& r) {
+      const uint8_t* p = a.kv4 + r.v;
+#pragma unroll
+      for (int d = 0; d < DT / 4; ++d) vs[d] = *(const uint32_t*)(p + vs_off + d * 4);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[d] = *(const u32x4*)(p + v_off + d * 256);
+    };
+    // The loads of a block's K are issued when the block before has its probabilities (the scores' registers are free then), those of V
+    // behind its second product: they travel while the wave, and the SIMD's other one, work on what lies between.
+    int k0 = key_of(unit);
+    Recs cur = records(k0, entries(k0));
+    Ent ahead = entries(key_of(unit + U));
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(cur);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(cur);
+    __builtin_amdgcn_sched_barrier(0);
     for (int i = unit; i < n_blk4; i += U) {
-      const int g0 = block_at(i) << 2, k0 = g0 << 5;
-      bool ok0, ok1, okv;
-      const uint8_t *r0 = record(g0 + gk, e0, ok0), *r1 = record(g0 + 2 + gk, e1, ok1), *rv = record(g0 + g, ev, okv);
-      u32x4 kf[8], vf[DT];
-      uint32_t ks[2], vs[DT / 4];
-#pragma unroll
-      for (int t = 0; t < 8; ++t) kf[t] = *(const u32x4*)((t < 4 ? r0 : r1) + k_off + (t & 3) * 4 * (DH / 2));
-      ks[0] = *(const uint32_t*)(r0 + ks_off);
-      ks[1] = *(const uint32_t*)(r1 + ks_off);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) vf[d] = *(const u32x4*)(rv + v_off + d * 256);
-#pragma unroll
-      for (int d = 0; d < DT / 4; ++d) vs[d] = *(const uint32_t*)(rv + vs_off + d * 4);
-      {
-        const int g1 = block_at(min(i + U, n_blk4 - 1)) << 2;
-        e0 = entry(g1 + gk); e1 = entry(g1 + 2 + gk); ev = entry(g1 + g);
-      }
-      // groups of which no key is read, or that cannot be: anything may lie there
-      const int kg = k0 + 32 * g;
-      const bool want = kg < n4 && read_any(kg, kg + 32), dead = !(want && okv);
-      bad |= want && !okv;
-      const uint64_t dead_m = __builtin_amdgcn_ballot_w64(dead);
       f32x4 s[8][QT];
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
+      for (int t = 0; t < 8; t += 2) {                          // (two tiles at a time: the second products wait for the first)
 #pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-          acc = mfma4_sel(t & 3, kf[t], qh[x], acc, ks[t >> 2], qs[x]);
-          if constexpr (DH == 128) acc = mfma4_sel(t & 3, kf[t], ql[x], acc, ks[t >> 2], qs[x] >> 8);
-          s[t][x] = acc;
-        }
-      if (dead_m != 0 || !read_all(k0, k0 + 128)) {
+        for (int y = t; y < t + 2; ++y)
+#pragma unroll
+          for (int x = 0; x < QT; ++x) s[y][x] = mfma4_sel(y & 3, kf[y], qh[x], f32x4{0.f, 0.f, 0.f, 0.f}, ks[y >> 2], qs[x]);
+        if constexpr (DH == 128)
+#pragma unroll
+          for (int y = t; y < t + 2; ++y)
+#pragma unroll
+            for (int x = 0; x < QT; ++x) s[y][x] = mfma4_sel(y & 3, kf[y], ql[x], s[y][x], ks[y >> 2], qs[x] >> 8);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const int k1 = key_of(i + U);
+      const Recs nxt = records(k1, ahead);
+      ahead = entries(key_of(i + 2 * U));
+      if (cur.dead != 0 || !read_all(k0, k0 + 128)) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-          const bool gone = (dead_m >> (16 * (2 * (t >> 2) + (g >> 1)))) & 1;
+          const bool gone = (cur.dead >> (2 * (t >> 2) + (g >> 1))) & 1;
 #pragma unroll
           for (int x = 0; x < QT; ++x)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int key = k0 + 64 * (t >> 2) + 16 * g + 4 * (t & 3) + e;
-              if (gone || !(key < a.n_sink || key > wlo[x])) s[t][x][e] = -DEV_INF;
+              const int at = 64 * (t >> 2) + 4 * (t & 3) + e;   // key = k0 + 16 g + at
+              const bool see = (bool)((at < a.n_sink - k0 - 16 * g) | (at > wlo[x] - k0 - 16 * g)) & !gone;
+              s[t][x][e] = see ? s[t][x][e] : -DEV_INF;
             }
         }
-        if (dead) {
+        const bool gone = (cur.dead >> g) & 1;
 #pragma unroll
-          for (int d = 0; d < DT; ++d) vf[d] = u32x4{0, 0, 0, 0};
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int d = 0; d < DT / 4; ++d) vs[d] = 0x7f7f7f7fu;
-        }
+          for (int e = 0; e < 4; ++e) vf[d][e] = gone ? 0u : vf[d][e];
+#pragma unroll
+        for (int d = 0; d < DT / 4; ++d) vs[d] = gone ? 0x7f7f7f7fu : vs[d];
       }
       attend_softmax<8, DT, QT>(s, a.scale_log2, m_run, l_run, oacc);
+      i32x8 ph[QT], pl[QT];
 #pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        i32x8 ph, pl;
+      for (int x = 0; x < QT; ++x)
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
           int h, l;
           e4m3_pair(s[t][x][0], s[t][x][1], s[t][x][2], s[t][x][3], h, l);
-          ph[t] = h;
-          pl[t] = l;
+          ph[x][t] = h;
+          pl[x][t] = l;
         }
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(nxt);                                              // (behind the last block: that one again)
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          oacc[d][x] = mfma4_sel(d & 3, vf[d], ph, oacc[d][x], vs[d >> 2], 127);
-          oacc[d][x] = mfma4_sel(d & 3, vf[d], pl, oacc[d][x], vs[d >> 2], 123);
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          oacc[d][x] = mfma4_sel(d & 3, vf[d], ph[x], oacc[d][x], vs[d >> 2], 127);
+          oacc[d][x] = mfma4_sel(d & 3, vf[d], pl[x], oacc[d][x], vs[d >> 2], 123);
         }
-      }
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(nxt);
+      __builtin_amdgcn_sched_barrier(0);
+      cur = nxt;
+      k0 = k1;
     }
   }
 
-  // ---- keys in bfloat16, blocks of 32, two at a time; the units go on behind the ones that took the last blocks of 128
-  if (active) {
-    const int f16 = n4 >> 5;
-    const int sB = max(lo, n4) >> 5, n_b = ((kv_len + 31) >> 5) - sB;
-    const int n_a = min(max(0, ((n_head + 31) >> 5) - f16), sB - f16), n_blk = n_a + n_b;
-    auto block_at = [&](int i) { return i < n_a ? f16 + i : sB + (i - n_a); };
+  // ---- keys in bfloat16, blocks of 32; the units go on behind the ones that took the last blocks of 128
+  const int f16 = n4 >> 5;
+  const int sB = max(lo, n4) >> 5, n_b16 = ((kv_len + 31) >> 5) - sB;
+  const int n_a16 = min(max(0, ((n_head + 31) >> 5) - f16), sB - f16), n_blk = n_a16 + n_b16;
+  int i = unit - n_blk4 % U;
+  if (i < 0) i += U;
+  if (active && i < n_blk) {
     const bf16_t *kslab = (const bf16_t*)a.k, *vslab = (const bf16_t*)a.v;
-    const int32_t* const table = a.table + (int64_t)b * a.max_pages;
+    const const_i32 table = (const_i32)(uintptr_t)(a.table + (int64_t)b * a.max_pages);
     u32x4 qf[QT][KK];
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) qf[t][kk] = *(const u32x4*)(q + (int64_t)row_in[t] * DH + kk * 32 + g * 8);
-    struct Blk { u32x4 kf[2][KK], vf[DT]; bool dead; };
-    auto page_of = [&](int key) { return a.pt_shift >= 0 ? key >> a.pt_shift : key / a.pt; };
-    auto entry = [&](int key) { const int pi = page_of(key), e = table[min(pi, a.max_pages - 1)]; return pi < a.max_pages ? e : -1; };
-    auto issue = [&](int kb, int ek, int ev, Blk& x) {
-      const int k0 = kb << 5, key_k = k0 + 8 * (c >> 2), key_v = k0 + 8 * g;     // (8 consecutive keys lie in one page)
-      const bool okk = (uint32_t)ek < (uint32_t)a.n_pages, okv = (uint32_t)ev < (uint32_t)a.n_pages;
-      const bool want = key_v < kv_len && read_any(key_v, key_v + 8);
-      x.dead = !(want && okv);
-      bad |= want && !okv;
-      const bf16_t* kp = kslab + (((int64_t)(okk ? ek : 0) * a.Hkv + kvh) * a.pt + (key_k - page_of(key_k) * a.pt) + (c & 3)) * DH + g * 8;
+    // A block's four pieces of 8 keys, each in one page: where the lane's piece of K and of V lies in the slabs, and which of them have
+    // no key that is read or cannot be addressed.
+    struct Ent { int e0, e1, e2, e3; };
+    struct Pcs { int64_t k, v; uint32_t dead; };
+    auto key_of = [&](int i) { const int j = min(i, n_blk - 1); return (j < n_a16 ? f16 + j : sB + (j - n_a16)) << 5; };
+    auto page_of = [&](int key) { return (int)__umulhi((uint32_t)key, a.pt_inv); };
+    auto entry = [&](int key) { return table[min(page_of(key), a.max_pages - 1)]; };
+    auto entries = [&](int k0) { return Ent{entry(k0), entry(k0 + 8), entry(k0 + 16), entry(k0 + 24)}; };
+    auto piece = [&](int key, int page, uint32_t bit, uint32_t& dead, int64_t& v) -> int64_t {
+      const int pi = page_of(key), slot = key - pi * a.pt;
+      const bool ok = (pi < a.max_pages) & ((uint32_t)page < (uint32_t)a.n_pages), want = (key < kv_len) & read_any(key, key + 8);
+      bad |= want & !ok;
+      dead |= want & ok ? 0u : bit;
+      const int64_t rows = ((int64_t)(ok ? page : 0) * a.Hkv + kvh) * a.pt;
+      v = rows * DH + slot;
+      return (rows + slot) * DH;
+    };
+    auto pieces = [&](int k0, const Ent& x) {
+      Pcs r;
+      uint32_t dead = 0;
+      int64_t v0, v1, v2, v3;
+      const int64_t r0 = piece(k0, x.e0, 1, dead, v0), r1 = piece(k0 + 8, x.e1, 2, dead, v1), r2 = piece(k0 + 16, x.e2, 4, dead, v2),
+                    r3 = piece(k0 + 24, x.e3, 8, dead, v3);
+      const int64_t ka = c & 4 ? r1 : r0, kb = c & 4 ? r3 : r2, va = g & 1 ? v1 : v0, vb = g & 1 ? v3 : v2;
+      r.k = c & 8 ? kb : ka;
+      r.v = g & 2 ? vb : va;
+      r.dead = dead;
+      return r;
+    };
+    u32x4 kf[2][KK], vf[DT];
+    // key 8 (c / 4) + c % 4 + 4 tt of the block is row c of score tile tt
+    auto load_k = [&](const Pcs& r) {
+      const bf16_t* kp = kslab + (r.k + (c & 3) * DH + g * 8);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) x.kf[tt][kk] = *(const u32x4*)(kp + tt * 4 * DH + kk * 32);
-      const bf16_t* vp = vslab + (((int64_t)(okv ? ev : 0) * a.Hkv + kvh) * DH + c) * a.pt + (key_v - page_of(key_v) * a.pt);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) x.vf[d] = *(const u32x4*)(vp + (int64_t)d * 16 * a.pt);
+        for (int kk = 0; kk < KK; ++kk) kf[tt][kk] = *(const u32x4*)(kp + tt * 4 * DH + kk * 32);
     };
-    auto zero_keys = [&](u32x4 (&vf)[DT], int k0, auto gone) {                   // V of the lane's keys for which gone(key)
+    auto load_v = [&](const Pcs& r) {
+      const bf16_t* vp = vslab + (r.v + c * a.pt);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[d] = *(const u32x4*)(vp + (int64_t)d * 16 * a.pt);
+    };
+    auto zero_keys = [&](u32x4 (&v)[DT], auto gone) {            // V of the lane's keys 8g + e for which gone(e)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int key = k0 + 8 * g + 2 * e;
-        const uint32_t m = (gone(key) ? 0u : 0xffffu) | (gone(key + 1) ? 0u : 0xffff0000u);
+        const uint32_t m = (gone(2 * e) ? 0u : 0xffffu) | (gone(2 * e + 1) ? 0u : 0xffff0000u);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) vf[d][e] &= m;
+        for (int d = 0; d < DT; ++d) v[d][e] &= m;
       }
     };
-    auto compute = [&](int kb, Blk& x) {
-      const int k0 = kb << 5;
+    int k0 = key_of(i);
+    Pcs cur = pieces(k0, entries(k0));
+    Ent ahead = entries(key_of(i + U));
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(cur);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(cur);
+    __builtin_amdgcn_sched_barrier(0);
+    for (; i < n_blk; i += U) {
       f32x4 s[2][QT];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
@@ -459,31 +526,38 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
         for (int t = 0; t < QT; ++t) {
           f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int kk = 0; kk < KK; ++kk) acc = mfma16(x.kf[tt][kk], qf[t][kk], acc);
+          for (int kk = 0; kk < KK; ++kk) acc = mfma16(kf[tt][kk], qf[t][kk], acc);
           s[tt][t] = acc;
         }
+      const int k1 = key_of(i + U);
+      const Pcs nxt = pieces(k1, ahead);
+      ahead = entries(key_of(i + 2 * U));
       bool apart = false;                                       // some rows do not read a value that is not finite
-      if (__builtin_amdgcn_ballot_w64(x.dead) != 0 || k0 + 32 > kv_len || !read_all(k0, k0 + 32)) {
+      const bool all = read_all(k0, k0 + 32);
+      if (cur.dead != 0 || k0 + 32 > kv_len || !all) {
+        const bool gone = (cur.dead >> g) & 1;
+        const int end = gone ? 0 : kv_len - k0 - 8 * g;         // the lane's keys 8g + e, e < end, are there
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int t = 0; t < QT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int key = k0 + 8 * g + 4 * tt + e;
-              if (x.dead || key >= kv_len || !(key < a.n_sink || key > wlo[t])) s[tt][t][e] = -DEV_INF;
+              const int at = 4 * tt + e;
+              const bool see = (bool)((at < a.n_sink - k0 - 8 * g) | (at > wlo[t] - k0 - 8 * g)) & (at < end);
+              s[tt][t][e] = see ? s[tt][t][e] : -DEV_INF;
             }
-        zero_keys(x.vf, k0, [&](int key) { return x.dead || key >= kv_len; });
-        if (!read_all(k0, k0 + 32)) {
-          bool odd = false;
+        zero_keys(vf, [&](int e) { return e >= end; });
+        if (!all) {
+          uint32_t odd = 0;
 #pragma unroll
           for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const uint32_t v = x.vf[d][e];
-              odd |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+              const uint32_t v = vf[d][e];
+              odd |= (uint32_t)((v & 0x7f80u) == 0x7f80u) | (uint32_t)((v & 0x7f800000u) == 0x7f800000u);
             }
-          apart = __builtin_amdgcn_ballot_w64(odd) != 0;
+          apart = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
         }
       }
       attend_softmax<2, DT, QT>(s, a.scale_log2, m_run, l_run, oacc);
@@ -497,54 +571,46 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
           ph[t][e] = h;
           pl[t][e] = pack_bf16x2(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
         }
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(nxt);
+      __builtin_amdgcn_sched_barrier(0);
       if (!apart) {
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
           for (int t = 0; t < QT; ++t) {
-            oacc[d][t] = mfma16(x.vf[d], ph[t], oacc[d][t]);
-            oacc[d][t] = mfma16(x.vf[d], pl[t], oacc[d][t]);
+            oacc[d][t] = mfma16(vf[d], ph[t], oacc[d][t]);
+            oacc[d][t] = mfma16(vf[d], pl[t], oacc[d][t]);
           }
       } else {
         // 0 * NaN is NaN: one query at a time, with the values it does not read taken out
 #pragma unroll
         for (int t = 0; t < QT; ++t)
           for (int cc = 0; cc < 16; ++cc) {
-            const int wl = __shfl(wlo[t], cc, 64);
-            u32x4 v[DT], h, l;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) v[d] = x.vf[d];
-            zero_keys(v, k0, [&](int key) { return !(key < a.n_sink || key > wl); });
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { h[e] = c == cc ? ph[t][e] : 0u; l[e] = c == cc ? pl[t][e] : 0u; }
+            const int wl = __shfl(wlo[t], cc, 64) - k0 - 8 * g, hd = a.n_sink - k0 - 8 * g;
+            const bool mine = c == cc;
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-              f32x4 o = mfma16(v[d], h, oacc[d][t]);
-              o = mfma16(v[d], l, o);
-              if (c == cc) oacc[d][t] = o;                      // (the other columns got 0 * NaN)
+              u32x4 v, h, l;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t m = ((2 * e < hd) | (2 * e > wl) ? 0xffffu : 0u) | ((2 * e + 1 < hd) | (2 * e + 1 > wl) ? 0xffff0000u : 0u);
+                v[e] = vf[d][e] & m;
+                h[e] = mine ? ph[t][e] : 0u;
+                l[e] = mine ? pl[t][e] : 0u;
+              }
+              f32x4 o = mfma16(v, h, oacc[d][t]);
+              o = mfma16(v, l, o);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[d][t][e] = mine ? o[e] : oacc[d][t][e];   // (the other columns got 0 * NaN)
             }
           }
       }
-    };
-    int i = unit - n_blk4 % U;
-    if (i < 0) i += U;
-    int ka = 0, va = 0, kb2 = 0, vb = 0;
-    auto entries = [&](int i, int& ek, int& ev) {
-      const int k0 = block_at(max(0, min(i, n_blk - 1))) << 5;
-      ek = entry(k0 + 8 * (c >> 2));
-      ev = entry(k0 + 8 * g);
-    };
-    entries(i, ka, va);
-    entries(i + U, kb2, vb);
-    for (; i < n_blk; i += 2 * U) {
-      const bool two = i + U < n_blk;
-      Blk x, y;
-      issue(block_at(i), ka, va, x);
-      issue(block_at(two ? i + U : i), two ? kb2 : ka, two ? vb : va, y);   // (a repeat of the first block's loads)
-      entries(i + 2 * U, ka, va);
-      entries(i + 3 * U, kb2, vb);
-      compute(block_at(i), x);
-      if (two) compute(block_at(i + U), y);
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(nxt);
+      __builtin_amdgcn_sched_barrier(0);
+      cur = nxt;
+      k0 = k1;
     }
   }
 
@@ -558,8 +624,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     l_red[t] = l;
   }
   auto store = [&](int d, int t, f32x4 v, float m, float l) {
-    const int64_t ro = row_out[t];
-    if (ro < 0) return;
+    if (rg * 16 * QT + t * 16 + c >= R) return;
+    const int64_t ro = row_in[t];
     const int ch = d * 16 + 4 * g;
     if (a.n_parts > 1) {
       const int64_t slot = ro * a.n_parts + blockIdx.z;
@@ -624,7 +690,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
       // (statistics of the parts go with channel tile 0, whose wave they belong to)
     }
   }
-  if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
+  if (bad && lane == 0) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
+  if (sq.bad && threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
 }
 
 // Partial results of a row: four channels a lane.
@@ -666,10 +733,13 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
   a.B = g.B; a.Q = g.Q; a.Hq = f.n_q_heads; a.Hkv = f.n_kv_heads; a.max_prefix = g.max_kv - g.Q;
   a.window = g.view->window; a.n_sink = g.view->n_sink;
   a.pt = f.page_tokens; a.max_pages = f.max_pages_per_seq; a.n_pages = f.n_pages; a.n_pages4 = c->n_pages4;
-  a.pt_shift = -1;
-  for (int sh = 5; sh < 31; ++sh) if (f.page_tokens == 1 << sh) a.pt_shift = sh;
+  a.pt_inv = 0;
   a.status = WSM(c, status, int32_t);
-  if (f.dtype == DLLM_BF16 && c->kernel_mode == 0 && f.page_tokens % 8 == 0 && c->map.attn_rows > 0) {
+  // (the division by multiplication is exact for positions below 2^32 / page_tokens, for any with a page size of a power of two)
+  const bool pow2 = (f.page_tokens & (f.page_tokens - 1)) == 0;
+  if (f.dtype == DLLM_BF16 && c->kernel_mode == 0 && f.page_tokens % 8 == 0 && c->map.attn_rows > 0 &&
+      (pow2 || (int64_t)f.max_pages_per_seq * f.page_tokens < (((int64_t)1 << 32) - 1) / f.page_tokens - 256)) {
+    a.pt_inv = (uint32_t)((((uint64_t)1 << 32) + f.page_tokens - 1) / f.page_tokens);
     const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, c->map.attn_rows);
     a.n_rg_wg = p.n_rg_wg; a.kspl = p.kspl; a.n_parts = p.n_parts;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)f.head_dim);
