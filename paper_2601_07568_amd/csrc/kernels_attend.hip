@@ -15,7 +15,7 @@ struct AttendArgs {
   uint32_t pt_inv;          // key / pt = the high word of key * pt_inv (k_attend)
   int32_t* status;
   // k_attend
-  int n_rg_wg, kspl;        // row groups of a workgroup, its waves along the keys of each
+  int kspl;                 // waves of a workgroup, along the keys of its row group
   int n_parts;              // workgroups along the keys; > 1: partial results, merged by k_attend_merge
   float scale_log2;         // log2(e) / sqrt(dh)
   float *part_o, *part_ml;  // [rows, n_parts, dh], [rows, n_parts, 2]
@@ -180,10 +180,12 @@ __device__ __forceinline__ f32x4 mfma4_sel(int sel, u32x4 a, i32x8 b, f32x4 c, u
 }
 // four floats -> four e4m3 (hi) and what they leave out, times 16, in e4m3 (lo)
 __device__ __forceinline__ void e4m3_pair(float x0, float x1, float x2, float x3, int& hi, int& lo) {
-  int h = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
+  int h;                                                        // (any register: the two conversions fill a half each)
+  s16x2 l;
+  asm volatile("" : "=v"(h), "=v"(l));
+  h = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, h, false);
   h = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, h, true);
   const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
-  s16x2 l = {0, 0};
   l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x0 - a[0], x1 - a[1], 0.0625f, false);
   l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, x2 - b[0], x3 - b[1], 0.0625f, true);
   hi = h;
@@ -234,18 +236,16 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int rw = w / a.kspl, kw = w - rw * a.kspl;             // row group and place along the keys inside the workgroup
-  const int rg = blockIdx.y * a.n_rg_wg + rw;
+  const int rg = blockIdx.y;
   const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv;
   const int G = a.Hq / a.Hkv;
   const AttendSeq sq = attend_seq(a, b);
   const int n_q = sq.n_q, R = n_q * G, kv_len = sq.kv_len, n4 = sq.n4;
-  if (blockIdx.y * a.n_rg_wg * 16 * QT >= R) {                 // (the whole workgroup)
-    if (sq.bad && threadIdx.x == 0 && blockIdx.y == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+  if (rg * 16 * QT >= R) {
+    if (sq.bad && threadIdx.x == 0 && rg == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
     return;
   }
-  const bool active = rg * 16 * QT < R;
-  const int U = a.n_parts * a.kspl, unit = blockIdx.z * a.kspl + kw;
+  const int U = a.n_parts * a.kspl, unit = blockIdx.z * a.kspl + w;
 
   // the lane's queries, and what the wave's rows read: [0, n_head) and [lo, kv_len), all of it from lo_all on
   int row_in[QT], wlo[QT];
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   int n_a = (min(n_head, n4) + 127) >> 7;
   if (n_b > 0) n_a = min(n_a, first);
   const int n_blk4 = n_a + n_b;
-  if (active && unit < n_blk4) {
+  if (unit < n_blk4) {
     i32x8 qh[QT], ql[DH == 128 ? QT : 1];
     uint32_t qs[QT];                                            // scale bytes: hi, lo in the next byte (DH 64: the lane's own)
 #pragma unroll
@@ -431,12 +431,17 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
       load_k(nxt);                                              // (behind the last block: that one again)
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; d += 2) {
 #pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          oacc[d][x] = mfma4_sel(d & 3, vf[d], ph[x], oacc[d][x], vs[d >> 2], 127);
-          oacc[d][x] = mfma4_sel(d & 3, vf[d], pl[x], oacc[d][x], vs[d >> 2], 123);
-        }
+        for (int y = d; y < d + 2; ++y)
+#pragma unroll
+          for (int x = 0; x < QT; ++x) oacc[y][x] = mfma4_sel(y & 3, vf[y], ph[x], oacc[y][x], vs[y >> 2], 127);
+#pragma unroll
+        for (int y = d; y < d + 2; ++y)
+#pragma unroll
+          for (int x = 0; x < QT; ++x) oacc[y][x] = mfma4_sel(y & 3, vf[y], pl[x], oacc[y][x], vs[y >> 2], 123);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       __builtin_amdgcn_sched_barrier(0);
       load_v(nxt);
       __builtin_amdgcn_sched_barrier(0);
@@ -451,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   const int n_a16 = min(max(0, ((n_head + 31) >> 5) - f16), sB - f16), n_blk = n_a16 + n_b16;
   int i = unit - n_blk4 % U;
   if (i < 0) i += U;
-  if (active && i < n_blk) {
+  if (i < n_blk) {
     const bf16_t *kslab = (const bf16_t*)a.k, *vslab = (const bf16_t*)a.v;
     const const_i32 table = (const_i32)(uintptr_t)(a.table + (int64_t)b * a.max_pages);
     u32x4 qf[QT][KK];
@@ -574,37 +579,48 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
       __builtin_amdgcn_sched_barrier(0);
       load_k(nxt);
       __builtin_amdgcn_sched_barrier(0);
-      if (!apart) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            oacc[d][t] = mfma16(vf[d], ph[t], oacc[d][t]);
-            oacc[d][t] = mfma16(vf[d], pl[t], oacc[d][t]);
-          }
-      } else {
-        // 0 * NaN is NaN: one query at a time, with the values it does not read taken out
+      if (apart) {
+        // 0 * NaN is NaN: what is not finite is taken out of V and added to the rows that read it.  Two products count, per channel
+        // and row, the values that are +infinity or NaN and those that are -infinity or NaN.
+        u32x4 see[QT];
 #pragma unroll
         for (int t = 0; t < QT; ++t)
-          for (int cc = 0; cc < 16; ++cc) {
-            const int wl = __shfl(wlo[t], cc, 64) - k0 - 8 * g, hd = a.n_sink - k0 - 8 * g;
-            const bool mine = c == cc;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              u32x4 v, h, l;
+          for (int e = 0; e < 4; ++e) {
+            const int hd = a.n_sink - k0 - 8 * g, wl = wlo[t] - k0 - 8 * g;
+            see[t][e] = ((2 * e < hd) | (2 * e > wl) ? 0x3f80u : 0u) | ((2 * e + 1 < hd) | (2 * e + 1 > wl) ? 0x3f800000u : 0u);
+          }
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t m = ((2 * e < hd) | (2 * e > wl) ? 0xffffu : 0u) | ((2 * e + 1 < hd) | (2 * e + 1 > wl) ? 0xffff0000u : 0u);
-                v[e] = vf[d][e] & m;
-                h[e] = mine ? ph[t][e] : 0u;
-                l[e] = mine ? pl[t][e] : 0u;
-              }
-              f32x4 o = mfma16(v, h, oacc[d][t]);
-              o = mfma16(v, l, o);
+        for (int d = 0; d < DT; ++d) {
+          u32x4 pos, neg;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) oacc[d][t][e] = mine ? o[e] : oacc[d][t][e];   // (the other columns got 0 * NaN)
+          for (int e = 0; e < 4; ++e) {
+            pos[e] = neg[e] = 0;
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+              const uint32_t v = (vf[d][e] >> (16 * hi)) & 0xffffu, m = v & 0x7fffu, one = 0x3f80u << (16 * hi);
+              pos[e] |= (m > 0x7f80u) | (v == 0x7f80u) ? one : 0u;
+              neg[e] |= (m > 0x7f80u) | (v == 0xff80u) ? one : 0u;
+              vf[d][e] &= m >= 0x7f80u ? ~(0xffffu << (16 * hi)) : 0xffffffffu;
             }
           }
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            const f32x4 np = mfma16(pos, see[t], f32x4{0.f, 0.f, 0.f, 0.f}), nn = mfma16(neg, see[t], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (np[e] > 0.f) oacc[d][t][e] += DEV_INF;
+              if (nn[e] > 0.f) oacc[d][t][e] -= DEV_INF;        // (both: NaN)
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) oacc[d][t] = mfma16(vf[d], ph[t], oacc[d][t]);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) oacc[d][t] = mfma16(vf[d], pl[t], oacc[d][t]);
       }
       __builtin_amdgcn_sched_barrier(0);
       load_v(nxt);
@@ -639,59 +655,53 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
   };
   if (a.kspl == 1) {
-    if (active)
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int d = 0; d < DT; ++d) store(d, t, oacc[d][t], m_run[t], l_red[t]);
   } else {
-    // the waves of a row group bring their sums to a common maximum and hand each other slices of the channels through LDS
-    const int KS = a.kspl;
-    float* sm_m = (float*)smem + rw * KS * QT * 32;             // [KS][QT][16] maxima, then sums
+    // the waves bring their sums to a common maximum and hand each other slices of the channels through LDS
+    const int KS = a.kspl;                                      // 2 or 4
+    float* sm_m = (float*)smem;                                 // [KS][QT][16] maxima, then sums
     float* sm_l = sm_m + KS * QT * 16;
-    f32x4* sm_o = (f32x4*)(smem + 4 * QT * 32 * sizeof(float)) + (int64_t)rw * UN * (KS - 1) * 64;   // [UN][KS - 1][64]
-    if (active && g == 0) {
+    f32x4* sm_o = (f32x4*)(smem + 4 * QT * 32 * sizeof(float)); // [UN][KS - 1][64]
+    if (g == 0) {
 #pragma unroll
-      for (int t = 0; t < QT; ++t) { sm_m[(kw * QT + t) * 16 + c] = m_run[t]; sm_l[(kw * QT + t) * 16 + c] = l_red[t]; }
+      for (int t = 0; t < QT; ++t) { sm_m[(w * QT + t) * 16 + c] = m_run[t]; sm_l[(w * QT + t) * 16 + c] = l_red[t]; }
     }
     __syncthreads();
     float m_all[QT], l_all[QT];
-    if (active) {
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float mx = -DEV_INF;
-        for (int k = 0; k < KS; ++k) mx = fmaxf(mx, sm_m[(k * QT + t) * 16 + c]);
-        const float base = mx > -DEV_INF ? mx : 0.f;
-        float ls = 0.f;
-        for (int k = 0; k < KS; ++k) ls = fmaf(sm_l[(k * QT + t) * 16 + c], __builtin_amdgcn_exp2f(sm_m[(k * QT + t) * 16 + c] - base), ls);
-        m_all[t] = mx;
-        l_all[t] = ls;
-        const float f = __builtin_amdgcn_exp2f(m_run[t] - base);
+    for (int t = 0; t < QT; ++t) {
+      float mx = -DEV_INF;
+      for (int k = 0; k < KS; ++k) mx = fmaxf(mx, sm_m[(k * QT + t) * 16 + c]);
+      const float base = mx > -DEV_INF ? mx : 0.f;
+      float ls = 0.f;
+      for (int k = 0; k < KS; ++k) ls = fmaf(sm_l[(k * QT + t) * 16 + c], __builtin_amdgcn_exp2f(sm_m[(k * QT + t) * 16 + c] - base), ls);
+      m_all[t] = mx;
+      l_all[t] = ls;
+      const float f = __builtin_amdgcn_exp2f(m_run[t] - base);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          oacc[d][t] = oacc[d][t] * f;
-          const int u = d * QT + t, own = u & (KS - 1);         // (KS is 2 or 4)
-          if (own != kw) sm_o[(u * (KS - 1) + ((kw - own - 1) & (KS - 1))) * 64 + lane] = oacc[d][t];
-        }
+      for (int d = 0; d < DT; ++d) {
+        oacc[d][t] = oacc[d][t] * f;
+        const int u = d * QT + t, own = u & (KS - 1);
+        if (own != w) sm_o[(u * (KS - 1) + ((w - own - 1) & (KS - 1))) * 64 + lane] = oacc[d][t];
       }
     }
     __syncthreads();
-    if (active) {
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const int u = d * QT + t;
-          if ((u & (KS - 1)) != kw) continue;
-          f32x4 v = oacc[d][t];
-          for (int k = 0; k < KS - 1; ++k) v = v + sm_o[(u * (KS - 1) + k) * 64 + lane];
-          store(d, t, v, m_all[t], l_all[t]);
-        }
-      // (statistics of the parts go with channel tile 0, whose wave they belong to)
-    }
+      for (int d = 0; d < DT; ++d) {
+        const int u = d * QT + t;
+        if ((u & (KS - 1)) != w) continue;
+        f32x4 v = oacc[d][t];
+        for (int k = 0; k < KS - 1; ++k) v = v + sm_o[(u * (KS - 1) + k) * 64 + lane];
+        store(d, t, v, m_all[t], l_all[t]);                     // (a part's statistics go with channel tile 0)
+      }
   }
   if (bad && lane == 0) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
-  if (sq.bad && threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+  if (sq.bad && threadIdx.x == 0 && rg == 0 && blockIdx.z == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
 }
 
 // Partial results of a row: four channels a lane.
@@ -741,13 +751,13 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
       (pow2 || (int64_t)f.max_pages_per_seq * f.page_tokens < (((int64_t)1 << 32) - 1) / f.page_tokens - 256)) {
     a.pt_inv = (uint32_t)((((uint64_t)1 << 32) + f.page_tokens - 1) / f.page_tokens);
     const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, c->map.attn_rows);
-    a.n_rg_wg = p.n_rg_wg; a.kspl = p.kspl; a.n_parts = p.n_parts;
+    a.kspl = p.kspl; a.n_parts = p.n_parts;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)f.head_dim);
     a.part_o = WSM(c, attn_part, float);
     a.part_ml = a.part_o + (size_t)c->map.attn_rows * f.head_dim;
-    const dim3 grid(g.B * f.n_kv_heads, p.n_chunks, p.n_parts);
-    const int threads = 64 * p.n_rg_wg * p.kspl;
-    const size_t lds = p.kspl == 1 ? 0 : (size_t)4 * p.qt * 32 * 4 + (size_t)p.n_rg_wg * (f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;
+    const dim3 grid(g.B * f.n_kv_heads, p.n_rg, p.n_parts);
+    const int threads = 64 * p.kspl;
+    const size_t lds = p.kspl == 1 ? 0 : (size_t)4 * p.qt * 32 * 4 + (size_t)(f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;
     if (f.head_dim == 128) {
       if (p.qt == 1) k_attend<128, 1><<<grid, threads, lds, s>>>(a);
       else k_attend<128, 2><<<grid, threads, lds, s>>>(a);

@@ -279,32 +279,32 @@ inline bool gt_qkv_fused(int cus, int M, int dq, int dkv, int dh, int K, int max
 
 // ---- attention over parts of the cache (k_attend)
 struct AttendPlan {
-  int qt;                   // 16-row tiles of a wave
-  int n_rg_wg, n_chunks;    // row groups (16 * qt rows) of a workgroup, workgroups along them
-  int kspl, n_parts;        // waves along the keys of a row group in a workgroup, workgroups along the keys
+  int qt, n_rg;             // 16-row tiles of a wave; row groups (16 * qt rows) of a (sequence, kv head), a workgroup each
+  int kspl, n_parts;        // waves of a workgroup (along the keys), workgroups along the keys
 };
-// max_kv: most keys of a sequence; four: most of them are in 4 bits
+// max_kv: most keys of a sequence; four: most of them are in 4 bits.
+// us by row groups a workgroup x waves along the keys of each x workgroups along the keys (four-wave workgroups):
+//   16 row groups, 777 keys in 4 bits (7 rows)          1x4x1 9.5    1x4x2 10.9   4x1x4 11.7
+//   32 row groups, 1056 keys in 4 bits                  1x4x1 15.3   1x4x3 14.6   4x1x6 16.5
+//   32 row groups, 1072 of bfloat16                     1x4x1 23.5   1x4x3 17.4   1x4x6 17.4   4x1x6 18.9
+//   512 row groups, up to 4160 in 4 bits                1x4x1 51.8   1x4x2 62.1   2x2x1 56.9   4x1x2 81.5
+//   896 row groups, up to 8224 in 4 bits                1x4x1 140    1x4x2 148    2x2x1 142    4x1x2 150
+// so: one row group a workgroup, parts along the keys only where a round of two workgroups a CU has room for them and a wave of
+// one workgroup would have more than three blocks of 128 keys or two of 32 (merging the parts is a launch: 2.5 us and more).
 inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int Q, int max_kv, int window, int n_sink, bool four, int64_t part_rows) {
   AttendPlan p{};
-  const int G = n_q_heads / n_kv_heads, rows = Q * G;
+  const int rows = Q * (n_q_heads / n_kv_heads);
   p.qt = rows <= 16 ? 1 : 2;
-  const int n_rg = (rows + 16 * p.qt - 1) / (16 * p.qt);
-  p.n_rg_wg = n_rg >= 3 ? 4 : n_rg;
-  p.n_chunks = (n_rg + p.n_rg_wg - 1) / p.n_rg_wg;
-  // most keys that a row group reads, in blocks of its walk
-  int64_t keys = max_kv;
+  p.n_rg = (rows + 16 * p.qt - 1) / (16 * p.qt);
+  int64_t keys = max_kv;                                      // most keys that a row group reads, in blocks of its walk
   if (window > 0 && (int64_t)window + Q + n_sink < keys) keys = (int64_t)window + Q + n_sink;
-  const int64_t blocks = four ? keys / 128 + 2 : keys / 32 + 1;
-  // two waves a SIMD; one wave may take a whole block
-  const int64_t groups = (int64_t)B * n_kv_heads * p.n_chunks * p.n_rg_wg;
-  int64_t units = (int64_t)cus * 8 / groups;
-  if (units > blocks) units = blocks;
-  if (units < 1) units = 1;
-  p.kspl = 4 / p.n_rg_wg;
-  if (p.kspl > units) p.kspl = units >= 2 ? 2 : 1;
-  p.n_parts = (int)((units + p.kspl - 1) / p.kspl);
-  if (p.n_parts > ATTN_MAX_SPLITS) p.n_parts = ATTN_MAX_SPLITS;
-  while (p.n_parts > 1 && (int64_t)p.n_parts * B * Q * n_q_heads > part_rows) --p.n_parts;
+  const int64_t blocks = four ? keys / 128 + 2 : (keys + 31) / 32, per = four ? 3 : 2;
+  p.kspl = blocks >= 3 ? 4 : (blocks == 2 ? 2 : 1);
+  const int64_t room = (int64_t)2 * cus / ((int64_t)B * n_kv_heads * p.n_rg), want = (blocks + 4 * per - 1) / (4 * per);
+  int64_t parts = room < want ? room : want;
+  if (parts > ATTN_MAX_SPLITS) parts = ATTN_MAX_SPLITS;
+  while (parts > 1 && parts * B * Q * n_q_heads > part_rows) --parts;
+  p.n_parts = parts > 1 ? (int)parts : 1;
   return p;
 }
 
