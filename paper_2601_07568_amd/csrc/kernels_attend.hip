@@ -750,23 +750,30 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
   if (f.dtype == DLLM_BF16 && c->kernel_mode == 0 && f.page_tokens % 8 == 0 && c->map.attn_rows > 0 &&
       (pow2 || (int64_t)f.max_pages_per_seq * f.page_tokens < (((int64_t)1 << 32) - 1) / f.page_tokens - 256)) {
     a.pt_inv = (uint32_t)((((uint64_t)1 << 32) + f.page_tokens - 1) / f.page_tokens);
-    const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, c->map.attn_rows);
-    a.kspl = p.kspl; a.n_parts = p.n_parts;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)f.head_dim);
     a.part_o = WSM(c, attn_part, float);
     a.part_ml = a.part_o + (size_t)c->map.attn_rows * f.head_dim;
-    const dim3 grid(g.B * f.n_kv_heads, p.n_rg, p.n_parts);
-    const int threads = 64 * p.kspl;
-    const size_t lds = p.kspl == 1 ? 0 : (size_t)4 * p.qt * 32 * 4 + (size_t)(f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;
-    if (f.head_dim == 128) {
-      if (p.qt == 1) k_attend<128, 1><<<grid, threads, lds, s>>>(a);
-      else k_attend<128, 2><<<grid, threads, lds, s>>>(a);
+    AttnPlan staged;
+    a.n_parts = attn_win_parts(c, g, &staged);
+    hipError_t e;
+    if (a.n_parts > 0) {
+      e = launch_attn_win(c, s, g, kv, staged, q, o, out_mt);
     } else {
-      if (p.qt == 1) k_attend<64, 1><<<grid, threads, lds, s>>>(a);
-      else k_attend<64, 2><<<grid, threads, lds, s>>>(a);
+      const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, c->map.attn_rows);
+      a.kspl = p.kspl; a.n_parts = p.n_parts;
+      const dim3 grid(g.B * f.n_kv_heads, p.n_rg, p.n_parts);
+      const int threads = 64 * p.kspl;
+      const size_t lds = p.kspl == 1 ? 0 : (size_t)4 * p.qt * 32 * 4 + (size_t)(f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;
+      if (f.head_dim == 128) {
+        if (p.qt == 1) k_attend<128, 1><<<grid, threads, lds, s>>>(a);
+        else k_attend<128, 2><<<grid, threads, lds, s>>>(a);
+      } else {
+        if (p.qt == 1) k_attend<64, 1><<<grid, threads, lds, s>>>(a);
+        else k_attend<64, 2><<<grid, threads, lds, s>>>(a);
+      }
+      e = hipGetLastError();
     }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.n_parts == 1) return e;
+    if (e != hipSuccess || a.n_parts == 1) return e;
     const int64_t rows = (int64_t)g.T * f.n_q_heads;
     if (f.head_dim == 128) k_attend_merge<128><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a, rows);
     else k_attend_merge<64><<<(unsigned)((rows + 15) / 16), 256, 0, s>>>(a, rows);

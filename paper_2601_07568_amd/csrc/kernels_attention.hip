@@ -36,6 +36,8 @@ struct AttnArgs {
   float* part_ml;           // [T*Hq, n_units, 2]
   int32_t* status;
 };
+// The staged kernel over parts of the cache: a row at position p reads keys below n_sink and those above p - window (0: all of them).
+struct AttnWinArgs : AttnArgs { int window, n_sink, max_prefix; };
 
 
 // Online softmax of one 32-key block for QT query tiles; the lane holds raw scores of keys
@@ -502,16 +504,25 @@ template <typename T>
 __device__ __forceinline__ void pin(T& x) { asm volatile("" : "+v"(x)); }
 template <typename T, typename U>
 __device__ __forceinline__ void pin(T& x, U& y) { asm volatile("" : "+v"(x), "+v"(y)); }
+// bytes of LDS in front of the page ids for blocks of which rows read different keys, and what such a call calls the first positions
+constexpr int dl_win_lds(int dh) { return 16 + 2 * 2 * dh * 8; }
+__device__ __forceinline__ int a_sink(const AttnArgs&) { return 0; }
+__device__ __forceinline__ int a_sink(const AttnWinArgs& a) { return a.n_sink; }
 // PG: 0 packed scratch; 1 paged, a 64-key block lies inside a page; 2 paged, smaller pages (a power of two of at least 8)
-template <int DH, int PG>
-__device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
+// A: AttnWinArgs (PG 1): only the blocks that some row of the sequence reads are walked, those of the first positions and those from
+// the first row's window on.  Where rows read different keys of a block its scores are masked row by row; values of such a block that
+// are not finite are taken out of V^T and added to the rows that read them (0 * NaN is NaN), by a bit per channel and key.  Rows behind
+// q_valid are not computed.
+template <int DH, int PG, typename A>
+__device__ __forceinline__ void attn_dl_body(const A& a) {
+  constexpr bool WIN = !std::is_same<A, AttnArgs>::value;
   constexpr int KK = DH / 16, DT = DH / 32, NM = KK + 4 * DT;   // score steps, channel tiles, products per half
   constexpr int NB = DL_NB, NW = 8;
   constexpr int NKF = DH / 8, NVF = DH / 8, NF = NKF + NVF, FPW = NF / NW;   // KiB of K, of V^T; copies of a wave
   static_assert(NKF % FPW == 0, "a wave's copies are K for all of a wave or V^T for all");
   constexpr int BLK = NF * 1024, nthr = NW * 64, KROW = DH * 2;
   extern __shared__ __attribute__((aligned(1024))) unsigned char dl_smem[];
-  int32_t* s_pg = (int32_t*)(dl_smem + NB * BLK);
+  int32_t* s_pg = (int32_t*)(dl_smem + NB * BLK + (WIN ? dl_win_lds(DH) : 0));
   const int tid = threadIdx.x;
   const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 31, h = lane >> 5;
@@ -520,9 +531,20 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
   const int b = blockIdx.z / a.Hkv, kvh = blockIdx.z - b * a.Hkv;
   const int G = a.Hq / a.Hkv;
   const int row_base = PG ? b * a.Q : a.cu[b];
-  const int n_q = PG ? a.Q : a.cu[b + 1] - a.cu[b];
+  int n_rows = PG ? a.Q : a.cu[b + 1] - a.cu[b], n_keys, pl = 0;
+  bool bad_len = false;
+  if constexpr (WIN) {
+    const int p = a.prefix_len[b];
+    pl = min(max(p, 0), a.max_prefix);
+    bad_len = pl != p;
+    n_rows = a.q_valid ? min(max(a.q_valid[b], 0), a.Q) : a.Q;
+    n_keys = pl + n_rows;
+    if (n_rows == 0 && bad_len && tid == 0 && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+  } else {
+    n_keys = PG ? a.prefix_len[b] + (a.q_valid ? min(max(a.q_valid[b], 0), a.Q) : a.Q) : n_rows;
+  }
+  const int n_q = n_rows, kv_len = n_keys;
   const int R = n_q * G;
-  const int kv_len = PG ? a.prefix_len[b] + (a.q_valid ? min(max(a.q_valid[b], 0), a.Q) : a.Q) : n_q;
   const bool active = w < a.n_rg_wg && rg * 32 < R;   // waves beyond the rows only help loading
   if (blockIdx.y * a.n_rg_wg * 32 >= R) return;              // whole workgroup beyond this sequence's rows
   if (PG && a.q_valid && a.q_valid[b] < 0) return;           // the sequence is not part of this call
@@ -532,7 +554,20 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
   const bf16_t* vslab = (const bf16_t*)kv.v;
   const int64_t pcol = PG ? 0 : kv.cu_pad[b];
   uint32_t bad = 0;
-  const int nkb = (kv_len + 63) >> 6;
+  // what the rows read: keys [0, n_head) and from lo on; all of them read keys below n_sink and from lo_all on.  In blocks: n_front of
+  // the first positions, then `skip` that nobody reads.
+  int lo = 0, lo_all = 0, n_head = 0, n_front = 0, skip = 0;
+  if constexpr (WIN) {
+    if (a.window > 0) {
+      lo = max(0, pl - a.window + 1);
+      lo_all = max(0, kv_len - a.window);
+      n_head = min(a.n_sink, lo);
+      n_front = min((n_head + 63) >> 6, lo >> 6);
+      skip = (lo >> 6) - n_front;
+    }
+  }
+  auto blk = [&](int j) { return WIN && j >= n_front ? j + skip : j; };
+  const int nkb = ((kv_len + 63) >> 6) - skip;
   const int n_own = unit < nkb ? (nkb - 1 - unit) / a.n_units + 1 : 0;   // the unit's blocks: unit, unit + n_units, ..
 
   int np = 0;
@@ -568,7 +603,7 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
   uint32_t badbuf = 0;                                        // PG 1: buffers with keys from a page id out of range
   // own: 0, 1, .. of the unit's blocks; past the last one it is the last one
   auto clampo = [&](int own) { return own < n_own ? own : n_own - 1; };
-  auto block_of = [&](int own) { return unit + clampo(own) * a.n_units; };
+  auto block_of = [&](int own) { return blk(unit + clampo(own) * a.n_units); };
   auto page_of = [&](int own) -> int {
     if constexpr (PG != 1) return 0;
     return s_pg[clampo(own)];
@@ -630,12 +665,13 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
   if (PG != 2 && n_own > 0) first_blocks();
   if constexpr (PG != 0)
     for (int i = tid; i < n_ids; i += nthr) {
-      const int pi = (((unit + (i >> ids_sh) * a.n_units) << 6) >> sh) + (i & ((1 << ids_sh) - 1));
+      const int pi = ((blk(unit + (i >> ids_sh) * a.n_units) << 6) >> sh) + (i & ((1 << ids_sh) - 1));
       s_pg[i] = pi < np ? table[pi] : -1;
     }
 
   u32x4 qf[KK];               // B operand: column r = the lane's query
   int64_t row_out;            // its (token * Hq + head), -1 if beyond R
+  int wlo = -1;               // (WIN) it reads the keys above this one
   {
     int rr = rg * 32 + r;
     const bool ok = active && rr < R;
@@ -643,6 +679,7 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
     const int hg = rr / n_q, j = rr - hg * n_q;
     const int64_t ro = (int64_t)(row_base + j) * a.Hq + kvh * G + hg;
     row_out = ok ? ro : -1;
+    if constexpr (WIN) wlo = a.window > 0 ? pl + j - a.window : -1;
     const bf16_t* qp = a.q + ro * DH + h * 8;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) qf[kk] = *(const u32x4*)(qp + kk * 16);
@@ -652,12 +689,18 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
     u32x4* vb = (u32x4*)(dl_smem + (NB - 1) * BLK + NKF * 1024);
     for (int q = tid; q < NVF * 64; q += nthr) vb[q] = u32x4{0, 0, 0, 0};
   }
+  // (WIN) of two blocks in turn: the block (own + 1) that has values that are not finite, and where: +infinity or NaN, -infinity or NaN
+  int32_t* const odd_own = (int32_t*)(dl_smem + NB * BLK);
+  uint8_t* const odd_at = dl_smem + NB * BLK + 16;            // [2 blocks][2 kinds][DH][8 bytes, a bit per key]
+  if (WIN && tid < 2) odd_own[tid] = 0;
+  auto edge = [&](int k64) { return !((k64 + 64 <= a_sink(a)) | (k64 >= lo_all)); };   // rows read different keys of it
   __syncthreads();                                            // page ids are in LDS
 
   // zeroes the V^T columns of keys past the sequence end and of keys without a page
   auto fix_tail = [&](int own, int buf) {
-    const int kb64 = unit + own * a.n_units;
+    const int kb64 = blk(unit + own * a.n_units);
     bool any = (kb64 << 6) + 64 > kv_len;
+    if constexpr (WIN) any |= edge(kb64 << 6);
     if constexpr (PG == 1) any |= (badbuf >> buf) & 1u;
     if constexpr (PG == 2) {
       for (int p = 0; p < 1 << ids_sh; ++p) any |= (uint32_t)s_pg[(own << ids_sh) + p] >= (uint32_t)kv.n_pages;
@@ -671,7 +714,26 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
       if constexpr (PG == 2) {
         if ((uint32_t)s_pg[(own << ids_sh) + ((key & 63) >> sh)] >= (uint32_t)kv.n_pages) valid = 0;
       }
-      if (valid < 8) {
+      if constexpr (WIN) {
+        const bool apart = edge(kb64 << 6);
+        u32x4 v = vb[q];
+        uint32_t pos = 0, neg = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t x = (v[e >> 1] >> (16 * (e & 1))) & 0xffffu, m = x & 0x7fffu;
+          const bool none = (e >= valid) | ((key + e >= n_head) & (key + e < lo)), odd = (bool)(apart & (m >= 0x7f80u)) & !none;
+          pos |= (uint32_t)(odd & ((m > 0x7f80u) | (x == 0x7f80u))) << e;
+          neg |= (uint32_t)(odd & ((m > 0x7f80u) | (x == 0xff80u))) << e;
+          if (none | odd) v[e >> 1] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+        }
+        vb[q] = v;
+        if (apart) {
+          uint8_t* const at = odd_at + ((own & 1) * 2 * DH + (q >> 3)) * 8 + ((q & 7) ^ ((q >> 4) & 7));
+          at[0] = (uint8_t)pos;
+          at[DH * 8] = (uint8_t)neg;
+          if (pos | neg) odd_own[own & 1] = own + 1;
+        }
+      } else if (valid < 8) {
         u32x4 v = vb[q];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -690,7 +752,8 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int e = 0; e < 16; ++e) oacc[d][e] = 0.f;
-  float m_run = -DEV_INF, l_run = 0.f, l_odd = 0.f;
+  // (WIN: a row may read nothing of a block; from a finite maximum its weights are 0)
+  float m_run = WIN ? -1e30f : -DEV_INF, l_run = 0.f, l_odd = 0.f;
   const float scl = a.scale_log2;
 
   struct Wts { u32x4 hi[2], lo[2]; };                         // weights of a half: B operands of its two steps
@@ -719,13 +782,21 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
   };
   const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
+  bool part = false;                                      // (WIN) of the current block: rows read different keys, or a page is missing
+  int cur_buf = 0;
   // in front of half k0's exponentials: mask, and now and then the new scale (mx: the scores' maximum, one per half wave)
   auto settle = [&](f32x16& s, float mx, int k0, Wts& open) {
-    if (k0 + 32 > kv_len) {                               // only a sequence's last block has keys to mask
+    if (k0 + 32 > kv_len || (WIN && part)) {              // only a sequence's last block has keys to mask
       mx = -DEV_INF;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        if (k0 + 16 * (e >> 3) + 8 * h + (e & 7) >= kv_len) s[e] = -DEV_INF;
+        const int key = k0 + 16 * (e >> 3) + 8 * h + (e & 7);
+        bool gone = key >= kv_len;
+        if constexpr (WIN) {
+          gone |= !((key < a.n_sink) | (key > wlo));
+          gone |= (badbuf >> cur_buf) & 1u;
+        }
+        if (gone) s[e] = -DEV_INF;
         mx = fmaxf(mx, s[e]);
       }
     }
@@ -867,7 +938,11 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
       for (int d = 0; d < DT; ++d) v0[d] = u32x4{0, 0, 0, 0};
     }
     for (int own = 0; own < n_own; ++own) {
-      const int kb = unit + own * a.n_units;
+      const int kb = blk(unit + own * a.n_units);
+      if constexpr (WIN) {
+        part = edge(kb << 6) | ((badbuf >> buf) & 1u);
+        cur_buf = buf;
+      }
       const int nbuf = buf == 0 ? NB - 1 : buf - 1;            // (buf + NB - 1) % NB: the buffer of the block before
       const int buf1 = buf + 1 == NB ? 0 : buf + 1;
       const int kn = block_of(own + NB - 1);
@@ -885,6 +960,21 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
         pg_next = page_of(own + NB);
         settle(sn, mx, (kb << 6) + 32, pa);
         mx = half_step(I0{}, I0{}, I1{}, I1{}, sn, sc, pb, pa, [&]() {}, [&](int) {});
+        if constexpr (WIN) {
+          if (part && odd_own[own & 1] == own + 1) {           // (written in front of this block's barrier, kept until the next but one)
+            const int k64 = kb << 6, hd = a.n_sink - k64, tl = wlo + 1 - k64;
+            const uint64_t see = (hd <= 0 ? 0ull : hd >= 64 ? ~0ull : (1ull << hd) - 1) | (tl <= 0 ? ~0ull : tl >= 64 ? 0ull : ~0ull << tl);
+            const uint64_t* const at = (const uint64_t*)(odd_at + (own & 1) * 2 * DH * 8);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const int ch = 32 * d + 8 * (e >> 2) + 4 * h + (e & 3);
+                if (at[ch] & see) oacc[d][e] += DEV_INF;
+                if (at[DH + ch] & see) oacc[d][e] -= DEV_INF;
+              }
+          }
+        }
       } else {
         turn();
 #pragma unroll
@@ -913,7 +1003,7 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
     l += __shfl_xor(l, 32, 64);
     if (row_out < 0) {
     } else if (a.n_units == 1) {
-      const float inv = l > 0.f ? 1.0f / l : 0.f;
+      const float inv = WIN || l > 0.f ? 1.0f / l : 0.f;
       const int tok = (int)(row_out / a.Hq), head = (int)(row_out - (int64_t)tok * a.Hq);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
@@ -936,11 +1026,14 @@ __device__ __forceinline__ void attn_dl_body(const AttnArgs& a) {
     }
   }
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
+  if (WIN && bad_len && tid == 0 && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
 }
 
 // (a kernel of its own around the body: as a kernel's own code it leaves the host without the launch stub)
 template <int DH, int PG>
 __global__ __launch_bounds__(512) void k_attn_dl(const AttnArgs a) { attn_dl_body<DH, PG>(a); }
+template <int DH>
+__global__ __launch_bounds__(512) void k_attn_dl_win(const AttnWinArgs a) { attn_dl_body<DH, 1>(a); }
 
 bool attn_step_supported(const dllm_ctx* c, const StepGeom& g) {
   const dllm_config& f = c->cfg;
@@ -960,6 +1053,8 @@ hipError_t init_attn_kernels() {
     e = hipFuncSetAttribute((const void*)k_attn_dl<DHV, PG>, hipFuncAttributeMaxDynamicSharedMemorySize, DL_LDS_MAX)
   DL_ATTR(128, 0); DL_ATTR(128, 1); DL_ATTR(128, 2); DL_ATTR(64, 0); DL_ATTR(64, 1); DL_ATTR(64, 2);
 #undef DL_ATTR
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)k_attn_dl_win<128>, hipFuncAttributeMaxDynamicSharedMemorySize, DL_LDS_MAX);
+  if (e == hipSuccess) e = hipFuncSetAttribute((const void*)k_attn_dl_win<64>, hipFuncAttributeMaxDynamicSharedMemorySize, DL_LDS_MAX);
   attn_merge_ready = e == hipSuccess;
   return e;
 }
@@ -1015,6 +1110,41 @@ hipError_t launch_attn_step(dllm_ctx* c, hipStream_t s, const StepGeom& g, const
     k_attn_combine<128><<<(rows + 3) / 4, 512, 0, s>>>(a.part_o, a.part_ml, a.n_parts, a.o, f.n_q_heads, a.out_mt, rows);
   else
     k_attn_combine<64><<<(rows + 7) / 8, 512, 0, s>>>(a.part_o, a.part_ml, a.n_parts, a.o, f.n_q_heads, a.out_mt, rows);
+  return hipGetLastError();
+}
+
+// The staged kernel over what g.view lets the rows read (nothing in 4 bits), for many rows a key head: parts along the keys that it
+// left in the workspace for the caller to merge (1: the output is written), 0: not for this call.
+int attn_win_parts(dllm_ctx* c, const StepGeom& g, AttnPlan* plan) {
+  const dllm_config& f = c->cfg;
+  if (g.view->len4 || !attn_step_supported(c, g) || f.page_tokens % 64 != 0) return 0;   // (with small pages the registers run out)
+  // most keys of the walk, in whole blocks of 64
+  int64_t keys = g.max_kv;
+  if (g.view->window > 0) {
+    const int64_t read = ((int64_t)g.view->n_sink + 63) / 64 * 64 + ((int64_t)g.view->window + g.Q + 126) / 64 * 64;
+    if (read < keys) keys = read;
+  }
+  *plan = attn_plan(device_cus(), f.head_dim, f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.T, (int)keys, f.page_tokens, c->map.attn_rows, attn_merge_ready);
+  return plan->staged && plan->lds + dl_win_lds(f.head_dim) <= (size_t)DL_LDS_MAX ? plan->units : 0;
+}
+hipError_t launch_attn_win(dllm_ctx* c, hipStream_t s, const StepGeom& g, const KVView& kv, const AttnPlan& p, const void* q, void* o, int out_mt) {
+  const dllm_config& f = c->cfg;
+  AttnWinArgs a;
+  a.q = (const bf16_t*)q; a.o = (bf16_t*)o; a.out_mt = out_mt;
+  a.prefix_len = g.prefix_len; a.q_valid = g.q_valid; a.cu = nullptr;
+  a.kv = kv;
+  a.Q = g.Q; a.Hq = f.n_q_heads; a.Hkv = f.n_kv_heads; a.B = g.B;
+  a.n_units = p.units; a.kspl = p.kspl; a.n_rg_wg = p.n_rg_wg; a.n_parts = p.units;
+  a.pt_shift = p.pt_shift; a.pg_cap = p.pg_cap;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)f.head_dim);
+  a.part_o = WSM(c, attn_part, float);
+  a.part_ml = a.part_o + (size_t)c->map.attn_rows * f.head_dim;
+  a.status = WSM(c, status, int32_t);
+  a.window = g.view->window; a.n_sink = g.view->n_sink; a.max_prefix = g.max_kv - g.Q;
+  const dim3 grid(p.units, p.n_chunks, g.B * f.n_kv_heads);
+  const size_t lds = p.lds + dl_win_lds(f.head_dim);
+  if (f.head_dim == 128) k_attn_dl_win<128><<<grid, 512, lds, s>>>(a);
+  else k_attn_dl_win<64><<<grid, 512, lds, s>>>(a);
   return hipGetLastError();
 }
 

@@ -291,6 +291,12 @@ CASES = [
     ("8/2x128", "bf16", [1000, 31], 32, None, None, 128, 0, 32),
     ("8/2x128", "bf16", [700], 64, [40], None, 31, 64, 7),
     ("28/4x128", "bf16", [500, 450], 32, None, None, 200, 5, 64),
+    ("28/4x128", "bf16", [500, 450, 3], 32, [32, 0, 17], None, 0, 0, 64),
+    ("28/4x128", "bf16", [700, 45], 64, [64, 33], None, 130, 70, 128),
+    ("28/4x128", "bf16", [640, 64], 40, None, None, 1, 0, 64),
+    ("28/4x128", "bf16", [333], 20, [-1], None, 40, 0, 64),
+    ("6/3x64", "bf16", [900, 130], 96, None, None, 100, 129, 64),
+    ("6/3x64", "bf16", [900, 130], 96, [90, 96], None, 1000, 3, 16),
     ("5/5x128", "bf16", [2000], 1, None, None, 0, 0, 64),
     ("5/5x128", "bf16", [2000], 3, None, None, 1999, 1, 128),
     ("6/3x64", "bf16", [32], 1, None, [32], 0, 0, 32),
@@ -314,37 +320,44 @@ def test_attend(i, mode):
 
 
 @pytest.mark.parametrize("four", [False, True])
-@pytest.mark.parametrize("Q", [1, 32])
-def test_attend_long(four, Q):
+@pytest.mark.parametrize("heads,Q", [("8/2x128", 1), ("8/2x128", 32), ("28/4x128", 32)])
+def test_attend_long(four, heads, Q):
     """Many parts along the keys, one sequence much longer than the others, a host bound that is longer still."""
-    Cache("8/2x128", "bf16", [9000, 40, 4097], Q, None, [9999] * 3 if four else None, 0, 0, 64, seed=5 + Q, slack=700).run().check()
+    Cache(heads, "bf16", [9000, 40, 4097], Q, None, [9999] * 3 if four else None, 0, 0, 64, seed=5 + Q, slack=700).run().check()
 
 
-@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("heads,pt,four", [("6/3x64", 16, False), ("6/3x64", 32, True), ("28/4x128", 64, False), ("28/4x128", 16, False)])
 @pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
-def test_what_is_not_read_does_not_reach_a_row(four, mode):
+def test_what_is_not_read_does_not_reach_a_row(heads, pt, four, mode):
     """Infinities and NaN in keys and values that some rows read and others do not: a row's output is what it would be without
-    those it does not read (and NaN where it reads a NaN)."""
-    c = Cache("6/3x64", "bf16", [200], 32, None, [64] if four else None, 60, 70, 16 if not four else 32, seed=1, mode=mode)
+    those it does not read, and not finite where it reads one."""
+    c = Cache(heads, "bf16", [200], 32, None, [64] if four else None, 60, 70, pt, seed=1, mode=mode)
     clean = c.run().out.clone()
     c.check()
-    # position 150 is read by rows whose p - 60 < 150: rows 0 .. 9 (p = 200 + j); 145 by rows 0 .. 4
-    pt = c.eng.cfg.page_tokens
-    for pos, val in ((150, float("nan")), (145, float("inf"))):
+    G = HEADS[heads][0] // HEADS[heads][1]
+    nan, inf = float("nan"), float("inf")
+    for pos, even, odd in ((150, nan, nan), (145, inf, inf), (158, -inf, None), (168, nan, inf)):   # (values of even and odd channels)
         page = c.table[0, pos // pt]
         row = c.eng.kv_slab(0, 1)[page, 1, pos % pt]
         keep = row.clone()
-        row.fill_(val)
+        row[::2] = even
+        if odd is not None:
+            row[1::2] = odd
+        hit = ~torch.isfinite(row)
         got = c.run().out
         row.copy_(keep)
         last = pos + 59 - 200                                               # the last row that reads it is at pos + 59
-        assert not torch.isfinite(got[0, :last + 1, 2:4]).any()             # its two query heads
+        mine = got[0, :, G:2 * G]                                           # the key head's query heads
+        assert not torch.isfinite(mine[:last + 1, :, hit]).any()
+        if even == even:
+            assert (mine[:last + 1, :, ::2] == even).all()
+        assert torch.equal(mine[:last + 1, :, ~hit], clean[0, :last + 1, G:2 * G][..., ~hit])
         assert torch.equal(got[0, last + 1:], clean[0, last + 1:])
-        assert torch.equal(got[0, :, :2], clean[0, :, :2]) and torch.equal(got[0, :, 4:], clean[0, :, 4:])
+        assert torch.equal(got[0, :, :G], clean[0, :, :G]) and torch.equal(got[0, :, 2 * G:], clean[0, :, 2 * G:])
     page = c.table[0, 160 // pt]
-    c.eng.kv_slab(0, 0)[page, 0, 160 % pt] = float("nan")                   # a key: rows 0 .. 19, heads 0 and 1
+    c.eng.kv_slab(0, 0)[page, 0, 160 % pt] = float("nan")                   # a key of head 0: rows 0 .. 19
     got = c.run().out
-    assert torch.isnan(got[0, :20, :2]).all() and torch.equal(got[0, 20:], clean[0, 20:])
+    assert torch.isnan(got[0, :20, :G]).all() and torch.equal(got[0, 20:], clean[0, 20:])
     assert c.eng.read_status() == 0
 
 
@@ -385,13 +398,15 @@ def test_nan_query_over_4_bits(mode):
 
 
 @pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("heads", ["6/3x64", "28/4x128"])
 @pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
-def test_bad_values_on_the_device(four, mode):
+def test_bad_values_on_the_device(four, heads, mode):
     """Prefix lengths beyond the host's bound and pages outside the pool are flagged; keys of such pages are left out; entries
     that map nothing that is read are not looked at."""
-    pt = 32
-    c = Cache("6/3x64", "bf16", [190, 150], 8, None, [64, 64] if four else None, 100, 20, pt, seed=8, mode=mode)
-    c.table[0, 0 if four else 1] = 12345                                    # (not read: in 4 bits / between sinks and window)
+    pt = 32 if four or heads == "6/3x64" else 64
+    c = Cache(heads, "bf16", [190, 150], 8 if heads == "6/3x64" else 24, None, [64, 64] if four else None, 100, 20, pt, seed=8, mode=mode)
+    if pt == 32:
+        c.table[0, 0 if four else 1] = 12345                                # (not read: in 4 bits / between sinks and window)
     c.run().check()
     c.table4[1, 1], keep = -9, c.table4[1, 1]
     if four:
@@ -399,19 +414,19 @@ def test_bad_values_on_the_device(four, mode):
         c.run()
         assert c.eng.read_status() == B.STATUS_BAD_PAGE
         c.eng.reset_status()
-        see = [j for j in range(158) if j < 20 or j >= 64]                  # what is left of the keys, for the row at 150 (51 .. 63 lost)
+        see = [j for j in range(len(c.k[1])) if j < 20 or j >= 64]          # what is left of the keys, for the row at 150 (51 .. 63 lost)
         ref, tol = R.attend(c.q[1, :1].double().numpy(), c.k[1][see], c.v[1][see], len(see) - 1, 0, 0, "bf16", 64)
         assert (np.abs(c.out[1, :1].double().cpu().numpy() - ref) <= tol).all()
         c.table4[1, 1] = keep
         c.kw["table4"] = c.eng.i32(c.table4)
-    keep = c.table[1, 4]
-    c.table[1, 4] = c.eng.cfg.n_pages                                       # positions 128 .. 157 of sequence 1
+    keep = c.table[1, 128 // pt]
+    c.table[1, 128 // pt] = c.eng.cfg.n_pages                               # the page of position 128 of sequence 1
     c.run()
     assert c.eng.read_status() == B.STATUS_BAD_PAGE
-    see = [j for j in range(158) if j < 20 or 51 <= j < 128]
+    see = [j for j in range(len(c.k[1])) if (j < 20 or 51 <= j) and not 128 <= j < 128 + pt]
     ref, tol = R.attend(c.q[1, :1].double().numpy(), c.k[1][see], c.v[1][see], len(see) - 1, 0, 0, "bf16", 64 if four else 0)
     assert (np.abs(c.out[1, :1].double().cpu().numpy() - ref) <= tol).all()
-    c.table[1, 4] = keep
+    c.table[1, 128 // pt] = keep
     for prefix, kw in (([191, 150], {}), ([-1, 150], {})):
         c.eng.reset_status()
         c.eng.attend(0, c.q.to(c.eng.device), c.eng.i32(prefix), c.eng.i32(c.table), c.out, **{**c.kw, "max_prefix_len": 190, **kw})
