@@ -192,13 +192,17 @@ __device__ __forceinline__ void e4m3_pair(float x0, float x1, float x2, float x3
   lo = __builtin_bit_cast(int, l);
 }
 
-// Probabilities are kept 2^8 times too large: the largest is then near the top of e4m3, and the sums divide it out again.
-constexpr float P_SHIFT = 8.0f;
+// Probabilities are kept 2^P_SHIFT times too large, and the running maximum follows the scores only when one exceeds it by more than
+// P_SLACK: with 16 rows a tile some row's maximum moves in nearly every block, which would rescale all sums each time.  The largest
+// probability is then 2^8, near the top of e4m3 (448); what lo resolves is 2^-13, 2^-17 of a row's largest at least.
+constexpr float P_SHIFT = 4.0f, P_SLACK = 4.0f;
 
 // Online softmax of NT score tiles (log2 units after scale_log2); s becomes the probabilities.  A row that has seen no key but
-// masked ones keeps the maximum -inf and weights 0.
-template <int NT, int DT, int QT>
-__device__ __forceinline__ void attend_softmax(f32x4 (&s)[NT][QT], float scale_log2, float (&m_run)[QT], float (&l_run)[QT], f32x4 (&oacc)[DT][QT]) {
+// masked ones keeps the maximum -inf and weights 0.  SUM: their sums go to l_run (else the caller has the matrix pipe add them up);
+// lsum is scaled with the outputs.
+template <bool SUM, int NT, int DT, int QT>
+__device__ __forceinline__ void attend_softmax(f32x4 (&s)[NT][QT], float scale_log2, float (&m_run)[QT], float (&l_run)[QT], f32x4 (&lsum)[QT],
+                                               f32x4 (&oacc)[DT][QT]) {
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     float mx = s[0][t][0];
@@ -206,17 +210,18 @@ __device__ __forceinline__ void attend_softmax(f32x4 (&s)[NT][QT], float scale_l
     for (int x = 0; x < NT; ++x)
 #pragma unroll
       for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[x][t][i]);
-    mx = rows_max(mx);
-    const float m_new = fmaxf(m_run[t], mx * scale_log2);
-    const float base = m_new > -DEV_INF ? m_new : 0.f;
-    if (__builtin_amdgcn_ballot_w64(m_new > m_run[t]) != 0) {
-      const float alpha = __builtin_amdgcn_exp2f(m_run[t] - base);
+    mx = rows_max(mx) * scale_log2;
+    // (a first finite score always moves it: -inf + P_SLACK)
+    if (__builtin_amdgcn_ballot_w64(mx > m_run[t] + P_SLACK) != 0) {
+      const float m_new = fmaxf(m_run[t], mx);
+      const float alpha = m_new > -DEV_INF ? __builtin_amdgcn_exp2f(m_run[t] - m_new) : 1.f;
       l_run[t] *= alpha;
+      lsum[t] = lsum[t] * alpha;
 #pragma unroll
       for (int d = 0; d < DT; ++d) oacc[d][t] = oacc[d][t] * alpha;
       m_run[t] = m_new;
     }
-    const float off = P_SHIFT - base;
+    const float off = P_SHIFT - (m_run[t] > -DEV_INF ? m_run[t] : 0.f);
     float ps = 0.f;
 #pragma unroll
     for (int x = 0; x < NT; ++x)
@@ -224,9 +229,9 @@ __device__ __forceinline__ void attend_softmax(f32x4 (&s)[NT][QT], float scale_l
       for (int i = 0; i < 4; ++i) {
         const float e = __builtin_amdgcn_exp2f(fmaf(s[x][t][i], scale_log2, off));
         s[x][t][i] = e;
-        ps += e;
+        if (SUM) ps += e;
       }
-    l_run[t] += ps;
+    if (SUM) l_run[t] += ps;
   }
 }
 
@@ -267,12 +272,13 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   auto read_all = [&](int k0, int k1) { return (bool)((k1 <= a.n_sink) | (k0 >= lo_all)); };     // every row reads keys k0 .. k1 - 1
   auto read_any = [&](int k0, int k1) { return (bool)((k0 < n_head) | (k1 > lo)); };             // some row may
 
-  f32x4 oacc[DT][QT];
-  float m_run[QT], l_run[QT];
+  f32x4 oacc[DT][QT], lsum[QT];               // lsum: the sum of the probabilities of keys in 4 bits, the same in all four
+  float m_run[QT], l_run[QT];                 // l_run: the lane's share of the others' sum
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     m_run[t] = -DEV_INF;
     l_run[t] = 0.f;
+    lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) oacc[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -416,7 +422,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
 #pragma unroll
         for (int d = 0; d < DT / 4; ++d) vs[d] = gone ? 0x7f7f7f7fu : vs[d];
       }
-      attend_softmax<8, DT, QT>(s, a.scale_log2, m_run, l_run, oacc);
+      attend_softmax<false, 8, DT, QT>(s, a.scale_log2, m_run, l_run, lsum, oacc);
       i32x8 ph[QT], pl[QT];
 #pragma unroll
       for (int x = 0; x < QT; ++x)
@@ -430,6 +436,12 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
       __builtin_amdgcn_sched_barrier(0);
       load_k(nxt);                                              // (behind the last block: that one again)
       __builtin_amdgcn_sched_barrier(0);
+      // (their sum: a row of ones - code 2 - in V's place)
+      const u32x4 ones = {0x22222222u, 0x22222222u, 0x22222222u, 0x22222222u};
+#pragma unroll
+      for (int x = 0; x < QT; ++x) lsum[x] = mfma4<0>(ones, ph[x], lsum[x], 127, 127);
+#pragma unroll
+      for (int x = 0; x < QT; ++x) lsum[x] = mfma4<0>(ones, pl[x], lsum[x], 127, 123);
 #pragma unroll
       for (int d = 0; d < DT; d += 2) {
 #pragma unroll
@@ -565,7 +577,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
           apart = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
         }
       }
-      attend_softmax<2, DT, QT>(s, a.scale_log2, m_run, l_run, oacc);
+      attend_softmax<true, 2, DT, QT>(s, a.scale_log2, m_run, l_run, lsum, oacc);
       u32x4 ph[QT], pl[QT];
 #pragma unroll
       for (int t = 0; t < QT; ++t)
@@ -637,7 +649,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     float l = l_run[t];
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
-    l_red[t] = l;
+    l_red[t] = l + lsum[t][0];
   }
   auto store = [&](int d, int t, f32x4 v, float m, float l) {
     if (rg * 16 * QT + t * 16 + c >= R) return;
