@@ -15,7 +15,7 @@ struct AttendArgs {
   uint32_t pt_inv;          // key / pt = the high word of key * pt_inv (k_attend)
   int32_t* status;
   // k_attend
-  int kspl;                 // waves of a workgroup, along the keys of its row group
+  int n_rg, kspl;           // row groups of a (sequence, key head); waves of a workgroup, along the keys of its row group
   int n_parts;              // workgroups along the keys; > 1: partial results, merged by k_attend_merge
   float scale_log2;         // log2(e) / sqrt(dh)
   float *part_o, *part_ml;  // [rows, n_parts, dh], [rows, n_parts, 2]
@@ -241,8 +241,10 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int rg = blockIdx.y;
-  const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv;
+  // the row groups of a (sequence, key head) one behind the other on one XCD, whose L2 then holds the keys for all of them
+  const int xi = blockIdx.x >> 3, seq = (xi / a.n_rg << 3) + (blockIdx.x & 7), rg = xi % a.n_rg;
+  if (seq >= a.B * a.Hkv) return;
+  const int b = seq / a.Hkv, kvh = seq - b * a.Hkv;
   const int G = a.Hq / a.Hkv;
   const AttendSeq sq = attend_seq(a, b);
   const int n_q = sq.n_q, R = n_q * G, kv_len = sq.kv_len, n4 = sq.n4;
@@ -250,7 +252,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     if (sq.bad && threadIdx.x == 0 && rg == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
     return;
   }
-  const int U = a.n_parts * a.kspl, unit = blockIdx.z * a.kspl + w;
+  const int U = a.n_parts * a.kspl, unit = blockIdx.y * a.kspl + w;
 
   // the lane's queries, and what the wave's rows read: [0, n_head) and [lo, kv_len), all of it from lo_all on
   int row_in[QT], wlo[QT];
@@ -656,7 +658,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     const int64_t ro = row_in[t];
     const int ch = d * 16 + 4 * g;
     if (a.n_parts > 1) {
-      const int64_t slot = ro * a.n_parts + blockIdx.z;
+      const int64_t slot = ro * a.n_parts + blockIdx.y;
       *(f32x4*)(a.part_o + slot * DH + ch) = v;
       if (d == 0 && g == 0) { a.part_ml[slot * 2] = m; a.part_ml[slot * 2 + 1] = l; }
       return;
@@ -713,7 +715,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
       }
   }
   if (bad && lane == 0) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
-  if (sq.bad && threadIdx.x == 0 && rg == 0 && blockIdx.z == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+  if (sq.bad && threadIdx.x == 0 && rg == 0 && blockIdx.y == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
 }
 
 // Partial results of a row: four channels a lane.
@@ -772,8 +774,8 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
       e = launch_attn_win(c, s, g, kv, staged, q, o, out_mt);
     } else {
       const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, c->map.attn_rows);
-      a.kspl = p.kspl; a.n_parts = p.n_parts;
-      const dim3 grid(g.B * f.n_kv_heads, p.n_rg, p.n_parts);
+      a.n_rg = p.n_rg; a.kspl = p.kspl; a.n_parts = p.n_parts;
+      const dim3 grid((g.B * f.n_kv_heads + 7) / 8 * 8 * p.n_rg, p.n_parts);
       const int threads = 64 * p.kspl;
       const size_t lds = p.kspl == 1 ? 0 : (size_t)4 * p.qt * 32 * 4 + (size_t)(f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;
       if (f.head_dim == 128) {
