@@ -168,6 +168,7 @@ class Engine:
         self._ws_off = (-self.workspace.data_ptr()) % 256
         self.kv_pool = torch.zeros(max(kv_bytes, 1), dtype=torch.uint8, device=self.device)
         self._lib, self._home = L, self.kv_pool.device
+        self._kv_typed = self.kv_pool.view(self.tdtype) if kv_bytes else None
         self.ctx = C.c_void_p()
         rc = L.dllm_create(C.byref(self.ctx), C.byref(self.cfg), C.byref(self._w), self.kv_pool.data_ptr(),
                            kv_bytes, self.workspace.data_ptr() + self._ws_off, ws_bytes)
@@ -210,7 +211,7 @@ class Engine:
         n = c.n_pages * c.n_kv_heads * c.page_tokens * c.head_dim
         off, pt, dh = (layer * 2 + which) * n, c.page_tokens, c.head_dim
         strides = (c.n_kv_heads * pt * dh, pt * dh, 1, pt) if which == 1 else (c.n_kv_heads * pt * dh, pt * dh, dh, 1)
-        return self.kv_pool.view(self.tdtype).as_strided((c.n_pages, c.n_kv_heads, pt, dh), strides, off)
+        return self._kv_typed.as_strided((c.n_pages, c.n_kv_heads, pt, dh), strides, off)
 
     # -- the calls of include/dllm.h
     def prefill_kv(self, tokens, cu_seqlens, block_table, n_cache=None, *, total_tokens, max_seqlen):

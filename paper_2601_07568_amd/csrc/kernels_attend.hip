@@ -15,6 +15,7 @@ struct AttendArgs {
   uint32_t pt_inv;          // key / pt = the high word of key * pt_inv (k_attend)
   int32_t* status;
   // k_attend
+  int lds_q;                // where a workgroup's LDS has its queries
   int n_rg, kspl;           // row groups of a (sequence, key head); waves of a workgroup, along the keys of its row group
   int n_parts;              // workgroups along the keys; > 1: partial results, merged by k_attend_merge
   float scale_log2;         // log2(e) / sqrt(dh)
@@ -197,42 +198,41 @@ __device__ __forceinline__ void e4m3_pair(float x0, float x1, float x2, float x3
 // probability is then 2^8, near the top of e4m3 (448); what lo resolves is 2^-13, 2^-17 of a row's largest at least.
 constexpr float P_SHIFT = 4.0f, P_SLACK = 4.0f;
 
-// Online softmax of NT score tiles (log2 units after scale_log2); s becomes the probabilities.  A row that has seen no key but
-// masked ones keeps the maximum -inf and weights 0.  SUM: their sums go to l_run (else the caller has the matrix pipe add them up);
-// lsum is scaled with the outputs.
-template <bool SUM, int NT, int DT, int QT>
-__device__ __forceinline__ void attend_softmax(f32x4 (&s)[NT][QT], float scale_log2, float (&m_run)[QT], float (&l_run)[QT], f32x4 (&lsum)[QT],
-                                               f32x4 (&oacc)[DT][QT]) {
+// Online softmax of one query tile's NT score tiles, in two steps: the maximum (log2 units after scale_log2), to which all sums are
+// brought where it moves, then the probabilities in the scores' place.  A row that has seen no key but masked ones keeps the maximum
+// -inf and weights 0.
+template <int NT, int DT, int QT>
+__device__ __forceinline__ void attend_max(const f32x4 (&s)[NT], int t, float scale_log2, float (&m_run)[QT], float (&l_run)[QT],
+                                           f32x4 (&oacc)[DT][QT]) {
+  float mx = s[0][0];
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    float mx = s[0][t][0];
+  for (int x = 0; x < NT; ++x)
 #pragma unroll
-    for (int x = 0; x < NT; ++x)
+    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[x][i]);
+  mx = rows_max(mx) * scale_log2;
+  // (a first finite score always moves it: -inf + P_SLACK)
+  if (__builtin_amdgcn_ballot_w64(mx > m_run[t] + P_SLACK) != 0) {
+    const float m_new = fmaxf(m_run[t], mx);
+    const float alpha = m_new > -DEV_INF ? __builtin_amdgcn_exp2f(m_run[t] - m_new) : 1.f;
+    l_run[t] *= alpha;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[x][t][i]);
-    mx = rows_max(mx) * scale_log2;
-    // (a first finite score always moves it: -inf + P_SLACK)
-    if (__builtin_amdgcn_ballot_w64(mx > m_run[t] + P_SLACK) != 0) {
-      const float m_new = fmaxf(m_run[t], mx);
-      const float alpha = m_new > -DEV_INF ? __builtin_amdgcn_exp2f(m_run[t] - m_new) : 1.f;
-      l_run[t] *= alpha;
-      lsum[t] = lsum[t] * alpha;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) oacc[d][t] = oacc[d][t] * alpha;
-      m_run[t] = m_new;
-    }
-    const float off = P_SHIFT - (m_run[t] > -DEV_INF ? m_run[t] : 0.f);
-    float ps = 0.f;
-#pragma unroll
-    for (int x = 0; x < NT; ++x)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[x][t][i], scale_log2, off));
-        s[x][t][i] = e;
-        if (SUM) ps += e;
-      }
-    if (SUM) l_run[t] += ps;
+    for (int d = 0; d < DT; ++d) oacc[d][t] = oacc[d][t] * alpha;
+    m_run[t] = m_new;
   }
+}
+template <int NT>
+__device__ __forceinline__ void attend_exp(f32x4 (&s)[NT], float scale_log2, float m, float& l) {
+  const float off = P_SHIFT - (m > -DEV_INF ? m : 0.f);
+  float p0 = 0.f, p1 = 0.f;
+#pragma unroll
+  for (int x = 0; x < NT; ++x)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[x][i] = __builtin_amdgcn_exp2f(fmaf(s[x][i], scale_log2, off));
+      if (i & 1) p1 += s[x][i];
+      else p0 += s[x][i];
+    }
+  l += p0 + p1;
 }
 
 template <int DH, int QT>
@@ -274,13 +274,12 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   auto read_all = [&](int k0, int k1) { return (bool)((k1 <= a.n_sink) | (k0 >= lo_all)); };     // every row reads keys k0 .. k1 - 1
   auto read_any = [&](int k0, int k1) { return (bool)((k0 < n_head) | (k1 > lo)); };             // some row may
 
-  f32x4 oacc[DT][QT], lsum[QT];               // lsum: the sum of the probabilities of keys in 4 bits, the same in all four
-  float m_run[QT], l_run[QT];                 // l_run: the lane's share of the others' sum
+  f32x4 oacc[DT][QT];
+  float m_run[QT], l_run[QT];                 // l_run: the lane's share of the sum
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     m_run[t] = -DEV_INF;
     l_run[t] = 0.f;
-    lsum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) oacc[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -292,11 +291,13 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   int n_a = (min(n_head, n4) + 127) >> 7;
   if (n_b > 0) n_a = min(n_a, first);
   const int n_blk4 = n_a + n_b;
-  if (unit < n_blk4) {
-    i32x8 qh[QT], ql[DH == 128 ? QT : 1];
-    uint32_t qs[QT];                                            // scale bytes: hi, lo in the next byte (DH 64: the lane's own)
+  // Their queries as e4m3 pairs, in LDS for all waves: as registers that live through the loop they would not fit.
+  u32x4* const sm_q = (u32x4*)(smem + a.lds_q);                // [QT][4: hi, hi, lo, lo (64 channels: hi, lo)][64]
+  uint32_t* const sm_qs = (uint32_t*)(sm_q + QT * 4 * 64);      // [QT][64] scale bytes: hi, lo in the next byte (64 channels: the lane's own)
+  if (n_blk4 > 0) {
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
+      if (t % a.kspl != w) continue;
       const bf16_t* p = q + (int64_t)row_in[t] * DH + 16 * g;
       uint32_t x[DH / 8];
 #pragma unroll
@@ -312,71 +313,84 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
       top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
       const uint32_t e = max(top >> 7, 12u);                    // the largest channel goes to 2^7 .. 2^8
       const float f = __uint_as_float((261u - e) << 23);
-      int h[DH / 16], l[DH / 16];
+      u32x4 h[DH / 64], l[DH / 64];
 #pragma unroll
-      for (int i = 0; i < DH / 16; ++i)
+      for (int i = 0; i < DH / 16; ++i) {
+        int hi, lo;
         e4m3_pair(__uint_as_float(x[2 * i] << 16) * f, __uint_as_float(x[2 * i] & 0xffff0000u) * f, __uint_as_float(x[2 * i + 1] << 16) * f,
-                  __uint_as_float(x[2 * i + 1] & 0xffff0000u) * f, h[i], l[i]);
-      if constexpr (DH == 128) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { qh[t][i] = h[i]; ql[t][i] = l[i]; }
-        qs[t] = (e - 7) | (e - 11) << 8;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { qh[t][i] = h[i]; qh[t][4 + i] = l[i]; }
-        qs[t] = g < 2 ? e - 7 : e - 11;
+                  __uint_as_float(x[2 * i + 1] & 0xffff0000u) * f, hi, lo);
+        h[i >> 2][i & 3] = (uint32_t)hi;
+        l[i >> 2][i & 3] = (uint32_t)lo;
       }
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i) {
+        sm_q[(t * 4 + i) * 64 + lane] = h[i];
+        sm_q[(t * 4 + DH / 64 + i) * 64 + lane] = l[i];
+      }
+      sm_qs[t * 64 + lane] = DH == 128 ? (e - 7) | (e - 11) << 8 : (g < 2 ? e - 7 : e - 11);
     }
+    __syncthreads();
+  }
+  if (unit < n_blk4) {
     const int gpp = a.pt >> 5;                                  // groups of 32 a page
     const const_i32 table = (const_i32)(uintptr_t)(a.table4 + (int64_t)b * a.max_pages);
     const int gch = DH == 128 ? g : g & 1;
-    const int k_off = (16 * ((c >> 2) & 1) + (c & 3)) * (DH / 2) + gch * 16, ks_off = 32 * DH + (((c >> 2) & 1) * 4 + (c & 3)) * (DH / 8) + gch * 4;
-    const int v_off = 16 * DH + c * 16, vs_off = 33 * DH + c * (DH / 16);
+    int k_off = (16 * ((c >> 2) & 1) + (c & 3)) * (DH / 2) + gch * 16, ks_off = 32 * DH + (((c >> 2) & 1) * 4 + (c & 3)) * (DH / 8) + gch * 4;
+    int v_off = 16 * DH + c * 16, vs_off = 33 * DH + c * (DH / 16);
     // A block's four records (scalar work): their bases, and which of them hold no key that is read or cannot be addressed - anything
     // may lie there.  Table entries are asked for a block ahead.
     struct Ent { int e0, e1, e2, e3; };
-    struct Recs { int64_t k0, k1, v; uint32_t dead; };          // the lane's: K of the first 64 keys, of the others, V
+    struct Recs { int k0, k1, v; uint32_t dead; };              // the lane's records: K of the first 64 keys, of the others, V
     auto key_of = [&](int i) { const int j = min(i, n_blk4 - 1); return (j < n_a ? j : first + (j - n_a)) << 7; };
     auto page_of = [&](int key) { return (int)__umulhi((uint32_t)key, a.pt_inv); };
     auto entry = [&](int key) { return table[min(page_of(key), a.max_pages - 1)]; };
     auto entries = [&](int k0) { return Ent{entry(k0), entry(k0 + 32), entry(k0 + 64), entry(k0 + 96)}; };
-    auto record = [&](int key, int page, uint32_t bit, uint32_t& dead) -> int64_t {
-      const int pi = page_of(key);
-      const bool ok = (pi < a.max_pages) & ((uint32_t)page < (uint32_t)a.n_pages4), want = (key < n4) & read_any(key, key + 32);
-      bad |= want & !ok;
-      dead |= want & ok ? 0u : bit;
-      return (((int64_t)(ok ? page : 0) * a.Hkv + kvh) * gpp + ((key - pi * a.pt) >> 5)) * (34 * DH);
-    };
     auto records = [&](int k0, const Ent& x) {
       Recs r;
-      uint32_t dead = 0;
-      const int64_t r0 = record(k0, x.e0, 1, dead), r1 = record(k0 + 32, x.e1, 2, dead), r2 = record(k0 + 64, x.e2, 4, dead),
-                    r3 = record(k0 + 96, x.e3, 8, dead);
+      int e0 = x.e0, e1 = x.e1, e2 = x.e2, e3 = x.e3;
+      r.dead = 0;
+      const uint32_t top = max(max((uint32_t)e0, (uint32_t)e1), max((uint32_t)e2, (uint32_t)e3));
+      if (top >= (uint32_t)a.n_pages4 || k0 + 128 > n4 || !(k0 + 128 <= n_head || k0 >= lo)) {
+        auto look = [&](int j, int& e) {
+          const int key = k0 + 32 * j;
+          const bool ok = (page_of(key) < a.max_pages) & ((uint32_t)e < (uint32_t)a.n_pages4), want = (key < n4) & read_any(key, key + 32);
+          bad |= want & !ok;
+          r.dead |= (uint32_t)!(want & ok) << j;
+          if (!ok) e = 0;
+        };
+        look(0, e0);
+        look(1, e1);
+        look(2, e2);
+        look(3, e3);
+      }
+      auto rec = [&](int j, int e) { const int key = k0 + 32 * j; return (e * a.Hkv + kvh) * gpp + ((key - page_of(key) * a.pt) >> 5); };
+      const int r0 = rec(0, e0), r1 = rec(1, e1), r2 = rec(2, e2), r3 = rec(3, e3);
       r.k0 = c & 8 ? r1 : r0;
       r.k1 = c & 8 ? r3 : r2;
-      const int64_t va = g & 1 ? r1 : r0, vb = g & 1 ? r3 : r2;
+      const int va = g & 1 ? r1 : r0, vb = g & 1 ? r3 : r2;
       r.v = g & 2 ? vb : va;
-      r.dead = dead;
       return r;
     };
     u32x4 kf[8], vf[DT];
     uint32_t ks[2], vs[DT / 4];
     auto load_k = [&](const Recs& r) {
-      const uint8_t *p0 = a.kv4 + (r.k0 + k_off), *p1 = a.kv4 + (r.k1 + k_off);
-      ks[0] = *(const uint32_t*)(p0 + (ks_off - k_off));
-      ks[1] = *(const uint32_t*)(p1 + (ks_off - k_off));
+      asm volatile("" : "+v"(k_off), "+v"(ks_off));             // (else the sums with the pool's address live through the loop)
+      const uint8_t *p0 = a.kv4 + (int64_t)r.k0 * (34 * DH), *p1 = a.kv4 + (int64_t)r.k1 * (34 * DH);
+      ks[0] = *(const uint32_t*)(p0 + ks_off);
+      ks[1] = *(const uint32_t*)(p1 + ks_off);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) kf[t] = *(const u32x4*)((t < 4 ? p0 : p1) + (t & 3) * 4 * (DH / 2));
+      for (int t = 0; t < 8; ++t) kf[t] = *(const u32x4*)((t < 4 ? p0 : p1) + k_off + (t & 3) * 4 * (DH / 2));
     };
     auto load_v = [&](const Recs& r) {
-      const uint8_t* p = a.kv4 + r.v;
+      asm volatile("" : "+v"(v_off), "+v"(vs_off));
+      const uint8_t* p = a.kv4 + (int64_t)r.v * (34 * DH);
 #pragma unroll
       for (int d = 0; d < DT / 4; ++d) vs[d] = *(const uint32_t*)(p + vs_off + d * 4);
 #pragma unroll
       for (int d = 0; d < DT; ++d) vf[d] = *(const u32x4*)(p + v_off + d * 256);
     };
-    // The loads of a block's K are issued when the block before has its probabilities (the scores' registers are free then), those of V
-    // behind its second product: they travel while the wave, and the SIMD's other one, work on what lies between.
+    // The loads of a block's K are issued when the block before has its scores, those of V behind its second product: they travel
+    // while the wave, and the SIMD's other one, work on what lies between.
     int k0 = key_of(unit);
     Recs cur = records(k0, entries(k0));
     Ent ahead = entries(key_of(unit + U));
@@ -386,36 +400,67 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     load_v(cur);
     __builtin_amdgcn_sched_barrier(0);
     for (int i = unit; i < n_blk4; i += U) {
-      f32x4 s[8][QT];
-#pragma unroll
-      for (int t = 0; t < 8; t += 2) {                          // (two tiles at a time: the second products wait for the first)
-#pragma unroll
-        for (int y = t; y < t + 2; ++y)
-#pragma unroll
-          for (int x = 0; x < QT; ++x) s[y][x] = mfma4_sel(y & 3, kf[y], qh[x], f32x4{0.f, 0.f, 0.f, 0.f}, ks[y >> 2], qs[x]);
-        if constexpr (DH == 128)
-#pragma unroll
-          for (int y = t; y < t + 2; ++y)
-#pragma unroll
-            for (int x = 0; x < QT; ++x) s[y][x] = mfma4_sel(y & 3, kf[y], ql[x], s[y][x], ks[y >> 2], qs[x] >> 8);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      const int k1 = key_of(i + U);
-      const Recs nxt = records(k1, ahead);
-      ahead = entries(key_of(i + 2 * U));
-      if (cur.dead != 0 || !read_all(k0, k0 + 128)) {
+      asm volatile("" ::: "memory");                            // (the queries are read again for every block)
+      // Matrix instructions of one query tile beside the vector instructions of the other: scores of tile 1 while tile 0's become
+      // probabilities, V^T P^T of tile 0 while tile 1's do.
+      f32x4 s[QT][8];
+      i32x8 ph[QT], pl[QT];
+      auto query = [&](int x, int part) {
+        const u32x4 u = sm_q[(x * 4 + 2 * part) * 64 + lane], v = sm_q[(x * 4 + 2 * part + 1) * 64 + lane];
+        return i32x8{(int)u[0], (int)u[1], (int)u[2], (int)u[3], (int)v[0], (int)v[1], (int)v[2], (int)v[3]};
+      };
+      // a product of the scores of tile x: n < 8 query hi with K tile n, behind it (128 channels) query lo with tile n - 8
+      uint32_t qs = 0;
+      i32x8 qh, ql;
+      auto ask_query = [&](int x) {
+        qs = sm_qs[x * 64 + lane];
+        qh = query(x, 0);
+        if constexpr (DH == 128) ql = query(x, 1);
+      };
+      auto score = [&](int x, int n) {
+        const int t = n & 7;
+        s[x][t] = n < 8 ? mfma4_sel(t & 3, kf[t], qh, f32x4{0.f, 0.f, 0.f, 0.f}, ks[t >> 2], qs)
+                        : mfma4_sel(t & 3, kf[t], ql, s[x][t], ks[t >> 2], qs >> 8);
+      };
+      const bool some = cur.dead != 0 || !read_all(k0, k0 + 128);
+      auto mask = [&](int x) {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
           const bool gone = (cur.dead >> (2 * (t >> 2) + (g >> 1))) & 1;
 #pragma unroll
-          for (int x = 0; x < QT; ++x)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int at = 64 * (t >> 2) + 4 * (t & 3) + e;   // key = k0 + 16 g + at
-              const bool see = (bool)((at < a.n_sink - k0 - 16 * g) | (at > wlo[x] - k0 - 16 * g)) & !gone;
-              s[t][x][e] = see ? s[t][x][e] : -DEV_INF;
-            }
+          for (int e = 0; e < 4; ++e) {
+            const int at = 64 * (t >> 2) + 4 * (t & 3) + e;     // key = k0 + 16 g + at
+            const bool see = (bool)((at < a.n_sink - k0 - 16 * g) | (at > wlo[x] - k0 - 16 * g)) & !gone;
+            s[x][t][e] = see ? s[x][t][e] : -DEV_INF;
+          }
         }
+      };
+      float off = 0.f;
+      auto weight_scale = [&](int x) { off = P_SHIFT - (m_run[x] > -DEV_INF ? m_run[x] : 0.f); };
+      auto weight = [&](int x, int t) {                         // score tile t becomes four bytes of the second product's operands
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[x][t][e], a.scale_log2, off));
+        l_run[x] += (p[0] + p[1]) + (p[2] + p[3]);
+        int h, l;
+        e4m3_pair(p[0], p[1], p[2], p[3], h, l);
+        asm volatile("" : "+v"(h), "+v"(l), "+v"(l_run[x]));    // (computed here, not where it is used)
+        ph[x][t] = h;
+        pl[x][t] = l;
+      };
+      auto output = [&](int x, int n) {                         // n < DT: P hi with channel tile n, behind it P lo with tile n - DT
+        const int d = n % DT;
+        oacc[d][x] = n < DT ? mfma4_sel(d & 3, vf[d], ph[x], oacc[d][x], vs[d >> 2], 127) : mfma4_sel(d & 3, vf[d], pl[x], oacc[d][x], vs[d >> 2], 123);
+      };
+      constexpr int NS = DH == 128 ? 16 : 8, NO = 2 * DT;       // products of a query tile's scores, of its outputs
+      ask_query(0);
+#pragma unroll
+      for (int n = 0; n < NS; ++n) score(0, n);
+      const int k1 = key_of(i + U);
+      const Recs nxt = records(k1, ahead);
+      ahead = entries(key_of(i + 2 * U));
+      if (some) {
+        mask(0);
         const bool gone = (cur.dead >> g) & 1;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -424,38 +469,40 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
 #pragma unroll
         for (int d = 0; d < DT / 4; ++d) vs[d] = gone ? 0x7f7f7f7fu : vs[d];
       }
-      attend_softmax<false, 8, DT, QT>(s, a.scale_log2, m_run, l_run, lsum, oacc);
-      i32x8 ph[QT], pl[QT];
-#pragma unroll
-      for (int x = 0; x < QT; ++x)
+      attend_max<8, DT, QT>(s[0], 0, a.scale_log2, m_run, l_run, oacc);
+      weight_scale(0);
+      if constexpr (QT == 2) {
+        ask_query(1);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
-          int h, l;
-          e4m3_pair(s[t][x][0], s[t][x][1], s[t][x][2], s[t][x][3], h, l);
-          ph[x][t] = h;
-          pl[x][t] = l;
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int n = t * NS / 8; n < (t + 1) * NS / 8; ++n) score(1, n);
+          weight(0, t);
         }
-      __builtin_amdgcn_sched_barrier(0);
-      load_k(nxt);                                              // (behind the last block: that one again)
-      __builtin_amdgcn_sched_barrier(0);
-      // (their sum: a row of ones - code 2 - in V's place)
-      const u32x4 ones = {0x22222222u, 0x22222222u, 0x22222222u, 0x22222222u};
+        __builtin_amdgcn_sched_barrier(0);
+        if (some) mask(1);
+        attend_max<8, DT, QT>(s[1], 1, a.scale_log2, m_run, l_run, oacc);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(nxt);                                            // (behind the last block: that one again)
+        weight_scale(1);
 #pragma unroll
-      for (int x = 0; x < QT; ++x) lsum[x] = mfma4<0>(ones, ph[x], lsum[x], 127, 127);
+        for (int t = 0; t < 8; ++t) {
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < QT; ++x) lsum[x] = mfma4<0>(ones, pl[x], lsum[x], 127, 123);
+          for (int n = t * NO / 8; n < (t + 1) * NO / 8; ++n) output(0, n);
+          weight(1, t);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
 #pragma unroll
-      for (int d = 0; d < DT; d += 2) {
-#pragma unroll
-        for (int y = d; y < d + 2; ++y)
-#pragma unroll
-          for (int x = 0; x < QT; ++x) oacc[y][x] = mfma4_sel(y & 3, vf[y], ph[x], oacc[y][x], vs[y >> 2], 127);
-#pragma unroll
-        for (int y = d; y < d + 2; ++y)
-#pragma unroll
-          for (int x = 0; x < QT; ++x) oacc[y][x] = mfma4_sel(y & 3, vf[y], pl[x], oacc[y][x], vs[y >> 2], 123);
+        for (int t = 0; t < 8; ++t) weight(0, t);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(nxt);
         __builtin_amdgcn_sched_barrier(0);
       }
+#pragma unroll
+      for (int n = 0; n < NO; ++n) output(QT - 1, n);
       __builtin_amdgcn_sched_barrier(0);
       load_v(nxt);
       __builtin_amdgcn_sched_barrier(0);
@@ -538,7 +585,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     load_v(cur);
     __builtin_amdgcn_sched_barrier(0);
     for (; i < n_blk; i += U) {
-      f32x4 s[2][QT];
+      f32x4 s[QT][2];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
@@ -546,7 +593,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
           f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int kk = 0; kk < KK; ++kk) acc = mfma16(kf[tt][kk], qf[t][kk], acc);
-          s[tt][t] = acc;
+          s[t][tt] = acc;
         }
       const int k1 = key_of(i + U);
       const Pcs nxt = pieces(k1, ahead);
@@ -564,7 +611,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
             for (int e = 0; e < 4; ++e) {
               const int at = 4 * tt + e;
               const bool see = (bool)((at < a.n_sink - k0 - 8 * g) | (at > wlo[t] - k0 - 8 * g)) & (at < end);
-              s[tt][t][e] = see ? s[tt][t][e] : -DEV_INF;
+              s[t][tt][e] = see ? s[t][tt][e] : -DEV_INF;
             }
         zero_keys(vf, [&](int e) { return e >= end; });
         if (!all) {
@@ -579,13 +626,16 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
           apart = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
         }
       }
-      attend_softmax<true, 2, DT, QT>(s, a.scale_log2, m_run, l_run, lsum, oacc);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) attend_max<2, DT, QT>(s[t], t, a.scale_log2, m_run, l_run, oacc);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) attend_exp<2>(s[t], a.scale_log2, m_run[t], l_run[t]);
       u32x4 ph[QT], pl[QT];
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p0 = s[e >> 1][t][(e & 1) * 2], p1 = s[e >> 1][t][(e & 1) * 2 + 1];
+          const float p0 = s[t][e >> 1][(e & 1) * 2], p1 = s[t][e >> 1][(e & 1) * 2 + 1];
           const uint32_t h = pack_bf16x2(p0, p1);
           ph[t][e] = h;
           pl[t][e] = pack_bf16x2(p0 - __uint_as_float(h << 16), p1 - __uint_as_float(h & 0xffff0000u));
@@ -651,7 +701,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     float l = l_run[t];
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
-    l_red[t] = l + lsum[t][0];
+    l_red[t] = l;
   }
   auto store = [&](int d, int t, f32x4 v, float m, float l) {
     if (rg * 16 * QT + t * 16 + c >= R) return;
@@ -761,7 +811,8 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
   a.status = WSM(c, status, int32_t);
   // (the division by multiplication is exact for positions below 2^32 / page_tokens, for any with a page size of a power of two)
   const bool pow2 = (f.page_tokens & (f.page_tokens - 1)) == 0;
-  if (f.dtype == DLLM_BF16 && c->kernel_mode == 0 && f.page_tokens % 8 == 0 && c->map.attn_rows > 0 &&
+  const bool records_fit = !a.len4 || (int64_t)c->n_pages4 * f.n_kv_heads * (f.page_tokens / 32) < ((int64_t)1 << 31);   // (numbered in 31 bits)
+  if (f.dtype == DLLM_BF16 && c->kernel_mode == 0 && f.page_tokens % 8 == 0 && c->map.attn_rows > 0 && records_fit &&
       (pow2 || (int64_t)f.max_pages_per_seq * f.page_tokens < (((int64_t)1 << 32) - 1) / f.page_tokens - 256)) {
     a.pt_inv = (uint32_t)((((uint64_t)1 << 32) + f.page_tokens - 1) / f.page_tokens);
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)f.head_dim);
@@ -777,7 +828,8 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
       a.n_rg = p.n_rg; a.kspl = p.kspl; a.n_parts = p.n_parts;
       const dim3 grid((g.B * f.n_kv_heads + 7) / 8 * 8 * p.n_rg, p.n_parts);
       const int threads = 64 * p.kspl;
-      const size_t lds = p.kspl == 1 ? 0 : (size_t)4 * p.qt * 32 * 4 + (size_t)(f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;
+      a.lds_q = p.kspl == 1 ? 0 : 4 * p.qt * 32 * 4 + (f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;   // (merging: statistics, sums)
+      const size_t lds = a.lds_q + (a.len4 ? p.qt * (4 * 1024 + 256) : 0);
       if (f.head_dim == 128) {
         if (p.qt == 1) k_attend<128, 1><<<grid, threads, lds, s>>>(a);
         else k_attend<128, 2><<<grid, threads, lds, s>>>(a);
