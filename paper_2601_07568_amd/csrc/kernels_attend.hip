@@ -235,42 +235,144 @@ __device__ __forceinline__ void attend_exp(f32x4 (&s)[NT], float scale_log2, flo
   l += p0 + p1;
 }
 
+// What a workgroup of k_attend / k_attend_f32 works on: row group rg (16 * QT rows) of (sequence b, kv head kvh), part `part` of the keys.
+struct AttendRows {
+  AttendSeq sq;
+  int b, kvh, rg, part, R;      // R: rows of the (sequence, kv head)
+  int lo, lo_all, n_head;       // its rows read keys [0, n_head) and from lo on; all of them those below n_sink and from lo_all on
+  bool none;                    // nothing to do
+};
+template <int QT>
+__device__ __forceinline__ AttendRows attend_rows(const AttendArgs& a) {
+  AttendRows v;
+  // the row groups of a part one behind the other on one XCD (workgroups go round over the eight), whose L2 then holds its keys for them
+  const int xi = blockIdx.x >> 3, u = (xi / a.n_rg << 3) + (blockIdx.x & 7), seq = u / a.n_parts;
+  v.rg = xi % a.n_rg;
+  v.part = u - seq * a.n_parts;
+  v.none = seq >= a.B * a.Hkv;
+  v.b = v.none ? 0 : seq / a.Hkv;
+  v.kvh = seq - v.b * a.Hkv;
+  v.sq = attend_seq(a, v.b);
+  v.R = v.sq.n_q * (a.Hq / a.Hkv);
+  v.none |= v.rg * 16 * QT >= v.R;
+  v.lo = v.lo_all = v.n_head = 0;
+  if (a.window > 0 && !v.none) {
+    const int n_q = v.sq.n_q, r0 = v.rg * 16 * QT, r1 = min(r0 + 16 * QT, v.R) - 1;
+    const bool one = r0 / n_q == r1 / n_q;
+    v.lo = max(0, v.sq.pl + (one ? r0 % n_q : 0) - a.window + 1);
+    v.lo_all = max(0, v.sq.pl + (one ? r1 % n_q : n_q - 1) - a.window + 1);
+    v.n_head = min(a.n_sink, v.lo);
+  }
+  return v;
+}
+// row (token * Hq + head) of the lane's query in tile t (of the last one beyond the end), and the position above which it reads keys
+__device__ __forceinline__ int attend_row(const AttendArgs& a, const AttendRows& v, int r, int& wlo) {
+  const int rr = min(r, v.R - 1), hg = rr / v.sq.n_q, j = rr - hg * v.sq.n_q;
+  wlo = a.window > 0 ? v.sq.pl + j - a.window : -1;
+  return (v.b * a.Q + j) * a.Hq + v.kvh * (a.Hq / a.Hkv) + hg;
+}
+__device__ __forceinline__ void attend_report(const AttendArgs& a, const AttendRows& v, bool bad) {
+  if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
+  if (v.sq.bad && threadIdx.x == 0 && v.rg == 0 && v.part == 0 && v.kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+}
+
+__device__ __forceinline__ void attend_put(const AttendArgs& a, int64_t row, int ch, int dh, f32x4 v, bf16_t*) {
+  const int tok = (int)(row / a.Hq), head = (int)(row - (int64_t)tok * a.Hq);
+  const int64_t at = a.out_mt > 0 ? frag_offset(tok, head * dh + ch, a.out_mt) : row * dh + ch;
+  *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+__device__ __forceinline__ void attend_put(const AttendArgs& a, int64_t row, int ch, int dh, f32x4 v, float*) {
+  *(f32x4*)((float*)a.o + row * dh + ch) = v;
+}
+
+// The end of a workgroup: the waves bring their sums to a common maximum and hand each other slices of the channels through LDS; then
+// the output, or this part's share of it.  The lane holds query column c, channels 16 d + 4g + i.
+template <typename T, int DH, int QT>
+__device__ __forceinline__ void attend_finish(const AttendArgs& a, const AttendRows& v, int lane, int w, unsigned char* smem, const int (&row_in)[QT],
+                                              f32x4 (&oacc)[DH / 16][QT], const float (&m_run)[QT], const float (&l_run)[QT]) {
+  constexpr int DT = DH / 16;
+  const int c = lane & 15, g = lane >> 4;
+  float l_red[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float l = l_run[t];
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    l_red[t] = l;
+  }
+  auto store = [&](int d, int t, f32x4 x, float m, float l) {
+    if (v.rg * 16 * QT + t * 16 + c >= v.R) return;
+    const int64_t ro = row_in[t];
+    const int ch = d * 16 + 4 * g;
+    if (a.n_parts > 1) {
+      const int64_t slot = ro * a.n_parts + v.part;
+      *(f32x4*)(a.part_o + slot * DH + ch) = x;
+      if (d == 0 && g == 0) { a.part_ml[slot * 2] = m; a.part_ml[slot * 2 + 1] = l; }
+      return;
+    }
+    const float inv = 1.0f / l;                                 // (no finite score: 0 / 0)
+    attend_put(a, ro, ch, DH, x * inv, (T*)nullptr);
+  };
+  if (a.kspl == 1) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) store(d, t, oacc[d][t], m_run[t], l_red[t]);
+    return;
+  }
+  const int KS = a.kspl;                                        // 2 or 4
+  float* sm_m = (float*)smem;                                   // [KS][QT][16] maxima, then sums
+  float* sm_l = sm_m + KS * QT * 16;
+  f32x4* sm_o = (f32x4*)(smem + 4 * QT * 32 * sizeof(float));   // [DT * QT][KS - 1][64]
+  if (g == 0) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) { sm_m[(w * QT + t) * 16 + c] = m_run[t]; sm_l[(w * QT + t) * 16 + c] = l_red[t]; }
+  }
+  __syncthreads();
+  float m_all[QT], l_all[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float mx = -DEV_INF;
+    for (int k = 0; k < KS; ++k) mx = fmaxf(mx, sm_m[(k * QT + t) * 16 + c]);
+    const float base = mx > -DEV_INF ? mx : 0.f;
+    float ls = 0.f;
+    for (int k = 0; k < KS; ++k) ls = fmaf(sm_l[(k * QT + t) * 16 + c], __builtin_amdgcn_exp2f(sm_m[(k * QT + t) * 16 + c] - base), ls);
+    m_all[t] = mx;
+    l_all[t] = ls;
+    const float f = __builtin_amdgcn_exp2f(m_run[t] - base);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      oacc[d][t] = oacc[d][t] * f;
+      const int u = d * QT + t, own = u & (KS - 1);
+      if (own != w) sm_o[(u * (KS - 1) + ((w - own - 1) & (KS - 1))) * 64 + lane] = oacc[d][t];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      const int u = d * QT + t;
+      if ((u & (KS - 1)) != w) continue;
+      f32x4 x = oacc[d][t];
+      for (int k = 0; k < KS - 1; ++k) x = x + sm_o[(u * (KS - 1) + k) * 64 + lane];
+      store(d, t, x, m_all[t], l_all[t]);                       // (a part's statistics go with channel tile 0)
+    }
+}
+
 template <int DH, int QT>
 __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
-  constexpr int KK = DH / 32, DT = DH / 16, UN = DT * QT;
+  constexpr int KK = DH / 32, DT = DH / 16;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
-  // the row groups of a (sequence, key head) one behind the other on one XCD, whose L2 then holds the keys for all of them
-  const int xi = blockIdx.x >> 3, seq = (xi / a.n_rg << 3) + (blockIdx.x & 7), rg = xi % a.n_rg;
-  if (seq >= a.B * a.Hkv) return;
-  const int b = seq / a.Hkv, kvh = seq - b * a.Hkv;
-  const int G = a.Hq / a.Hkv;
-  const AttendSeq sq = attend_seq(a, b);
-  const int n_q = sq.n_q, R = n_q * G, kv_len = sq.kv_len, n4 = sq.n4;
-  if (rg * 16 * QT >= R) {
-    if (sq.bad && threadIdx.x == 0 && rg == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
-    return;
-  }
-  const int U = a.n_parts * a.kspl, unit = blockIdx.y * a.kspl + w;
-
-  // the lane's queries, and what the wave's rows read: [0, n_head) and [lo, kv_len), all of it from lo_all on
+  const AttendRows v = attend_rows<QT>(a);
+  if (v.none) { attend_report(a, v, false); return; }
+  const int b = v.b, kvh = v.kvh, kv_len = v.sq.kv_len, n4 = v.sq.n4, lo = v.lo, lo_all = v.lo_all, n_head = v.n_head;
+  const int U = a.n_parts * a.kspl, unit = v.part * a.kspl + w;
   int row_in[QT], wlo[QT];
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int r = rg * 16 * QT + t * 16 + c, rr = min(r, R - 1);
-    const int hg = rr / n_q, j = rr - hg * n_q;
-    row_in[t] = (b * a.Q + j) * a.Hq + kvh * G + hg;
-    wlo[t] = a.window > 0 ? sq.pl + j - a.window : -1;         // keys above it are read
-  }
-  int lo = 0, lo_all = 0, n_head = 0;
-  if (a.window > 0) {
-    const int r0 = min(rg * 16 * QT, R - 1), r1 = min(rg * 16 * QT + 16 * QT, R) - 1;
-    const bool one = r0 / n_q == r1 / n_q;
-    lo = max(0, sq.pl + (one ? r0 % n_q : 0) - a.window + 1);
-    lo_all = max(0, sq.pl + (one ? r1 % n_q : n_q - 1) - a.window + 1);
-    n_head = min(a.n_sink, lo);
-  }
+  for (int t = 0; t < QT; ++t) row_in[t] = attend_row(a, v, v.rg * 16 * QT + t * 16 + c, wlo[t]);
   auto read_all = [&](int k0, int k1) { return (bool)((k1 <= a.n_sink) | (k0 >= lo_all)); };     // every row reads keys k0 .. k1 - 1
   auto read_any = [&](int k0, int k1) { return (bool)((k0 < n_head) | (k1 > lo)); };             // some row may
 
@@ -694,105 +796,183 @@ __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
     }
   }
 
-  // ---- results: the lane holds query column c, channels d*16 + 4g + i
-  float l_red[QT];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    float l = l_run[t];
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    l_red[t] = l;
-  }
-  auto store = [&](int d, int t, f32x4 v, float m, float l) {
-    if (rg * 16 * QT + t * 16 + c >= R) return;
-    const int64_t ro = row_in[t];
-    const int ch = d * 16 + 4 * g;
-    if (a.n_parts > 1) {
-      const int64_t slot = ro * a.n_parts + blockIdx.y;
-      *(f32x4*)(a.part_o + slot * DH + ch) = v;
-      if (d == 0 && g == 0) { a.part_ml[slot * 2] = m; a.part_ml[slot * 2 + 1] = l; }
-      return;
-    }
-    const float inv = 1.0f / l;                                 // (no finite score: 0 / 0)
-    const int tok = (int)(ro / a.Hq), head = (int)(ro - (int64_t)tok * a.Hq);
-    const int64_t at = a.out_mt > 0 ? frag_offset(tok, head * DH + ch, a.out_mt) : ro * DH + ch;
-    *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
-  };
-  if (a.kspl == 1) {
-#pragma unroll
-      for (int t = 0; t < QT; ++t)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) store(d, t, oacc[d][t], m_run[t], l_red[t]);
-  } else {
-    // the waves bring their sums to a common maximum and hand each other slices of the channels through LDS
-    const int KS = a.kspl;                                      // 2 or 4
-    float* sm_m = (float*)smem;                                 // [KS][QT][16] maxima, then sums
-    float* sm_l = sm_m + KS * QT * 16;
-    f32x4* sm_o = (f32x4*)(smem + 4 * QT * 32 * sizeof(float)); // [UN][KS - 1][64]
-    if (g == 0) {
-#pragma unroll
-      for (int t = 0; t < QT; ++t) { sm_m[(w * QT + t) * 16 + c] = m_run[t]; sm_l[(w * QT + t) * 16 + c] = l_red[t]; }
-    }
-    __syncthreads();
-    float m_all[QT], l_all[QT];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float mx = -DEV_INF;
-      for (int k = 0; k < KS; ++k) mx = fmaxf(mx, sm_m[(k * QT + t) * 16 + c]);
-      const float base = mx > -DEV_INF ? mx : 0.f;
-      float ls = 0.f;
-      for (int k = 0; k < KS; ++k) ls = fmaf(sm_l[(k * QT + t) * 16 + c], __builtin_amdgcn_exp2f(sm_m[(k * QT + t) * 16 + c] - base), ls);
-      m_all[t] = mx;
-      l_all[t] = ls;
-      const float f = __builtin_amdgcn_exp2f(m_run[t] - base);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        oacc[d][t] = oacc[d][t] * f;
-        const int u = d * QT + t, own = u & (KS - 1);
-        if (own != w) sm_o[(u * (KS - 1) + ((w - own - 1) & (KS - 1))) * 64 + lane] = oacc[d][t];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const int u = d * QT + t;
-        if ((u & (KS - 1)) != w) continue;
-        f32x4 v = oacc[d][t];
-        for (int k = 0; k < KS - 1; ++k) v = v + sm_o[(u * (KS - 1) + k) * 64 + lane];
-        store(d, t, v, m_all[t], l_all[t]);                     // (a part's statistics go with channel tile 0)
-      }
-  }
-  if (bad && lane == 0) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
-  if (sq.bad && threadIdx.x == 0 && rg == 0 && blockIdx.y == 0 && kvh == 0) atomicOr(a.status, DLLM_STATUS_BAD_LENGTH);
+  attend_finish<bf16_t, DH, QT>(a, v, lane, w, smem, row_in, oacc, m_run, l_run);
+  attend_report(a, v, bad && lane == 0);
 }
 
-// Partial results of a row: four channels a lane.
+// ==========================================================================================
+// Float models with pages of a multiple of 4 tokens: the same walk in blocks of 32 keys, 16 rows a wave, on the float matrix
+// instruction.  v_mfma_f32_16x16x4 (lane l, c = l % 16, g = l / 16): the first operand is row c, k = g, the second column c, k = g,
+// one float each; D is column c, rows 4g .. 4g+3.  k = g of score step (kk, e) is channel 16 kk + 4g + e, so that a lane's share of a row
+// of K or Q is 16-byte pieces; the scores of keys 4g + i are then step i of V^T P^T as they stand, and V^T's share keys 4g .. 4g+3.
+// Bound by a wave's chain of matrix instructions (64 channels: 64 of them a block, 0.9 us) and the latency of its loads.  Windows of 300
+// .. 4096 keys of 4 heads of 64 channels, 1 .. 32 sequences of 1 .. 96 rows: 11 .. 63 us where k_attend_any takes 190 .. 430.
 template <int DH>
+__global__ __launch_bounds__(256, 2) void k_attend_f32(const AttendArgs a) {
+  constexpr int KK = DH / 16, DT = DH / 16;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const AttendRows v = attend_rows<1>(a);
+  if (v.none) { attend_report(a, v, false); return; }
+  const int kv_len = v.sq.kv_len, lo = v.lo, lo_all = v.lo_all, n_head = v.n_head;
+  const int U = a.n_parts * a.kspl, unit = v.part * a.kspl + w;
+  int row_in[1], wlo;
+  row_in[0] = attend_row(a, v, v.rg * 16 + c, wlo);
+  auto read_all = [&](int k0, int k1) { return (bool)((k1 <= a.n_sink) | (k0 >= lo_all)); };
+  auto read_any = [&](int k0, int k1) { return (bool)((k0 < n_head) | (k1 > lo)); };
+  f32x4 oacc[DT][1], qf[KK];
+  float m_run[1] = {-DEV_INF}, l_run[1] = {0.f};
+  bool bad = false;
+#pragma unroll
+  for (int d = 0; d < DT; ++d) oacc[d][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) qf[kk] = *(const f32x4*)((const float*)a.q + (int64_t)row_in[0] * DH + 16 * kk + 4 * g);
+  const int sB = lo >> 5, n_a = min((n_head + 31) >> 5, sB), n_blk = n_a + ((kv_len + 31) >> 5) - sB;
+  const const_i32 table = (const_i32)(uintptr_t)(a.table + (int64_t)v.b * a.max_pages);
+  auto page_of = [&](int key) { return (int)__umulhi((uint32_t)key, a.pt_inv); };
+  auto mm = [&](float x, float y, f32x4 z) { return __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, z, 0, 0, 0); };
+  auto first_of = [&](int i) { return (i < n_a ? i : sB + (i - n_a)) << 5; };
+  int ek[2], ev[2];                                             // table entries of the block's K and V, requested a block ahead
+  auto entries = [&](int k0) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      ek[u] = table[min(page_of(k0 + 16 * u + c), a.max_pages - 1)];
+      ev[u] = table[min(page_of(k0 + 16 * u + 4 * g), a.max_pages - 1)];
+    }
+  };
+  if (unit < n_blk) entries(first_of(unit));
+  for (int i = unit; i < n_blk; i += U) {
+    const int k0 = first_of(i);
+    // K row k0 + 16 u + c, V^T columns k0 + 16 u + 4g .. +3 of half u; dead: none of these four keys is read, or they cannot be addressed
+    f32x4 kf[2][KK], vf[2][DT];
+    bool dead[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int key_k = k0 + 16 * u + c, key_v = k0 + 16 * u + 4 * g, pk = page_of(key_k), pv = page_of(key_v);
+      const bool okk = (pk < a.max_pages) & ((uint32_t)ek[u] < (uint32_t)a.n_pages), okv = (pv < a.max_pages) & ((uint32_t)ev[u] < (uint32_t)a.n_pages);
+      const bool want = (key_v < kv_len) & read_any(key_v, key_v + 4);
+      bad |= want & !okv;
+      dead[u] = !(want & okv);
+      const float* kp = (const float*)a.k + ((((int64_t)(okk ? ek[u] : 0) * a.Hkv + v.kvh) * a.pt + (key_k - pk * a.pt)) * DH + 4 * g);
+      const float* vp = (const float*)a.v + ((((int64_t)(okv ? ev[u] : 0) * a.Hkv + v.kvh) * DH + c) * a.pt + (key_v - pv * a.pt));
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) kf[u][kk] = *(const f32x4*)(kp + 16 * kk);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[u][d] = *(const f32x4*)(vp + (int64_t)d * 16 * a.pt);
+    }
+    if (i + U < n_blk) entries(first_of(i + U));
+    f32x4 s[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;                   // (two sums: half the chain)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        x = mm(kf[u][kk][0], qf[kk][0], x);
+        y = mm(kf[u][kk][1], qf[kk][1], y);
+        x = mm(kf[u][kk][2], qf[kk][2], x);
+        y = mm(kf[u][kk][3], qf[kk][3], y);
+      }
+      s[u] = x + y;
+    }
+    const bool all = read_all(k0, k0 + 32);
+    auto is = [&](int u, int e) { return (k0 + 16 * u + 4 * g + e < kv_len) & !dead[u]; };                  // a key there is
+    auto mine = [&](int u, int e) {                                                                        // ... that the lane's row reads
+      const int key = k0 + 16 * u + 4 * g + e;
+      return is(u, e) & ((key < a.n_sink) | (key > wlo));
+    };
+    if (__builtin_amdgcn_ballot_w64(dead[0] | dead[1]) != 0 || k0 + 32 > kv_len || !all) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[u][e] = mine(u, e) ? s[u][e] : -DEV_INF;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) vf[u][d][e] = is(u, e) ? vf[u][d][e] : 0.f;
+        }
+    }
+    attend_max<2, DT, 1>(s, 0, a.scale_log2, m_run, l_run, oacc);
+    if (!all) {
+      // 0 * NaN is NaN: what is not finite is taken out of V and added to the rows that read it (their number, by products)
+      bool odd = false;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd |= !(fabsf(vf[u][d][e]) < DEV_INF);
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          f32x4 np = {0.f, 0.f, 0.f, 0.f}, nn = np;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = vf[u][d][e], see = mine(u, e) ? 1.f : 0.f;
+              np = mm(x != x || x == DEV_INF ? 1.f : 0.f, see, np);
+              nn = mm(x != x || x == -DEV_INF ? 1.f : 0.f, see, nn);
+              vf[u][d][e] = fabsf(x) < DEV_INF ? x : 0.f;
+            }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (np[e] > 0.f) oacc[d][0][e] += DEV_INF;
+            if (nn[e] > 0.f) oacc[d][0][e] -= DEV_INF;
+          }
+        }
+      }
+    }
+    attend_exp<2>(s, a.scale_log2, m_run[0], l_run[0]);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) oacc[d][0] = mm(vf[u][d][e], s[u][e], oacc[d][0]);
+  }
+  attend_finish<float, DH, 1>(a, v, lane, w, smem, row_in, oacc, m_run, l_run);
+  attend_report(a, v, bad);
+}
+
+// Partial results of a row: four channels a lane, eight parts requested together.
+template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_attend_merge(const AttendArgs a, int64_t n_rows) {
   constexpr int LR = DH / 4;
   const int64_t row = (int64_t)blockIdx.x * (256 / LR) + threadIdx.x / LR;
   if (row >= n_rows) return;
   const int ch = threadIdx.x % LR * 4;
-  const int tok = (int)(row / a.Hq), head = (int)(row - (int64_t)tok * a.Hq), b = tok / a.Q;
+  const int tok = (int)(row / a.Hq), b = tok / a.Q;
   const int qv = a.q_valid ? a.q_valid[b] : a.Q;
   if (tok - b * a.Q >= qv) return;                               // (no partials of rows that are not part of the call)
-  const float* ml = a.part_ml + row * a.n_parts * 2;
+  const float2* ml = (const float2*)a.part_ml + row * a.n_parts;
   const float* po = a.part_o + row * a.n_parts * DH + ch;
-  float mx = -DEV_INF;
-  for (int p = 0; p < a.n_parts; ++p) mx = fmaxf(mx, ml[2 * p]);
-  const float base = mx > -DEV_INF ? mx : 0.f;
-  float den = 0.f;
+  float mx = -DEV_INF, den = 0.f;
   f32x4 num = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < a.n_parts; ++p) {
-    const float f = __builtin_amdgcn_exp2f(ml[2 * p] - base);
-    den = fmaf(ml[2 * p + 1], f, den);
-    num = num + *(const f32x4*)(po + (int64_t)p * DH) * f;
+  for (int p0 = 0; p0 < a.n_parts; p0 += 8) {
+    float2 x[8];
+    f32x4 o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = min(p0 + i, a.n_parts - 1);
+      x[i] = ml[p];
+      o[i] = *(const f32x4*)(po + (int64_t)p * DH);
+    }
+    float m = mx;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i].x);
+    const float base = m > -DEV_INF ? m : 0.f, r = __builtin_amdgcn_exp2f(mx - base);
+    den *= r;
+    num = num * r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p0 + i < a.n_parts) {
+        const float f = __builtin_amdgcn_exp2f(x[i].x - base);
+        den = fmaf(x[i].y, f, den);
+        num = num + o[i] * f;
+      }
+    mx = m;
   }
-  const float inv = 1.0f / den;
-  const int64_t at = a.out_mt > 0 ? frag_offset(tok, head * DH + ch, a.out_mt) : row * DH + ch;
-  *(uint2*)((bf16_t*)a.o + at) = make_uint2(pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv));
+  attend_put(a, row, ch, DH, num * (1.0f / den), (T*)nullptr);
 }
 
 hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int layer, const void* q, void* o, int out_mt) {
@@ -812,25 +992,31 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
   // (the division by multiplication is exact for positions below 2^32 / page_tokens, for any with a page size of a power of two)
   const bool pow2 = (f.page_tokens & (f.page_tokens - 1)) == 0;
   const bool records_fit = !a.len4 || (int64_t)c->n_pages4 * f.n_kv_heads * (f.page_tokens / 32) < ((int64_t)1 << 31);   // (numbered in 31 bits)
-  if (f.dtype == DLLM_BF16 && c->kernel_mode == 0 && f.page_tokens % 8 == 0 && c->map.attn_rows > 0 && records_fit &&
+  const bool bf16 = f.dtype == DLLM_BF16;
+  if (c->kernel_mode == 0 && f.page_tokens % (bf16 ? 8 : 4) == 0 && records_fit &&
       (pow2 || (int64_t)f.max_pages_per_seq * f.page_tokens < (((int64_t)1 << 32) - 1) / f.page_tokens - 256)) {
     a.pt_inv = (uint32_t)((((uint64_t)1 << 32) + f.page_tokens - 1) / f.page_tokens);
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)f.head_dim);
-    a.part_o = WSM(c, attn_part, float);
-    a.part_ml = a.part_o + (size_t)c->map.attn_rows * f.head_dim;
+    // float models have no buffer for partial results: theirs lie where the feed-forward product keeps its results (g, u, h), idle here
+    const int64_t part_rows = bf16 ? c->map.attn_rows : (int64_t)((c->map.rope_cos - c->map.g) / 4) / (f.head_dim + 2);
+    a.part_o = bf16 ? WSM(c, attn_part, float) : WSM(c, g, float);
+    a.part_ml = a.part_o + part_rows * f.head_dim;
     AttnPlan staged;
     a.n_parts = attn_win_parts(c, g, &staged);
     hipError_t e;
     if (a.n_parts > 0) {
       e = launch_attn_win(c, s, g, kv, staged, q, o, out_mt);
     } else {
-      const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, c->map.attn_rows);
+      const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, bf16, part_rows);
       a.n_rg = p.n_rg; a.kspl = p.kspl; a.n_parts = p.n_parts;
-      const dim3 grid((g.B * f.n_kv_heads + 7) / 8 * 8 * p.n_rg, p.n_parts);
+      const unsigned grid = (unsigned)(((int64_t)g.B * f.n_kv_heads * p.n_parts + 7) / 8 * 8 * p.n_rg);
       const int threads = 64 * p.kspl;
       a.lds_q = p.kspl == 1 ? 0 : 4 * p.qt * 32 * 4 + (f.head_dim / 16) * p.qt * (p.kspl - 1) * 1024;   // (merging: statistics, sums)
       const size_t lds = a.lds_q + (a.len4 ? p.qt * (4 * 1024 + 256) : 0);
-      if (f.head_dim == 128) {
+      if (!bf16) {
+        if (f.head_dim == 128) k_attend_f32<128><<<grid, threads, lds, s>>>(a);
+        else k_attend_f32<64><<<grid, threads, lds, s>>>(a);
+      } else if (f.head_dim == 128) {
         if (p.qt == 1) k_attend<128, 1><<<grid, threads, lds, s>>>(a);
         else k_attend<128, 2><<<grid, threads, lds, s>>>(a);
       } else {
@@ -841,8 +1027,14 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
     }
     if (e != hipSuccess || a.n_parts == 1) return e;
     const int64_t rows = (int64_t)g.T * f.n_q_heads;
-    if (f.head_dim == 128) k_attend_merge<128><<<(unsigned)((rows + 7) / 8), 256, 0, s>>>(a, rows);
-    else k_attend_merge<64><<<(unsigned)((rows + 15) / 16), 256, 0, s>>>(a, rows);
+    const unsigned n = (unsigned)((rows + 1024 / f.head_dim - 1) / (1024 / f.head_dim));
+    if (f.head_dim == 128) {
+      if (bf16) k_attend_merge<bf16_t, 128><<<n, 256, 0, s>>>(a, rows);
+      else k_attend_merge<float, 128><<<n, 256, 0, s>>>(a, rows);
+    } else {
+      if (bf16) k_attend_merge<bf16_t, 64><<<n, 256, 0, s>>>(a, rows);
+      else k_attend_merge<float, 64><<<n, 256, 0, s>>>(a, rows);
+    }
     return hipGetLastError();
   }
   if (f.dtype == DLLM_BF16) k_attend_any<bf16_t><<<dim3(g.T, f.n_q_heads), 256, 0, s>>>(a, f.head_dim);

@@ -291,10 +291,10 @@ struct AttendPlan {
 //   896 row groups, up to 8224 in 4 bits                1x4x1 140    1x4x2 148    2x2x1 142    4x1x2 150
 // so: one row group a workgroup, parts along the keys only where a round of two workgroups a CU has room for them and a wave of
 // one workgroup would have more than three blocks of 128 keys or two of 32 (merging the parts is a launch: 2.5 us and more).
-inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int Q, int max_kv, int window, int n_sink, bool four, int64_t part_rows) {
+inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int Q, int max_kv, int window, int n_sink, bool four, bool bf16, int64_t part_rows) {
   AttendPlan p{};
   const int rows = Q * (n_q_heads / n_kv_heads);
-  p.qt = rows <= 16 ? 1 : 2;
+  p.qt = rows <= 16 || !bf16 ? 1 : 2;
   p.n_rg = (rows + 16 * p.qt - 1) / (16 * p.qt);
   int64_t keys = max_kv;                                      // most keys that a row group reads, in blocks of its walk
   if (window > 0 && (int64_t)window + Q + n_sink < keys) keys = (int64_t)window + Q + n_sink;
