@@ -397,8 +397,8 @@ int dllm_refresh_cache(dllm_ctx *ctx, void *stream, int B, int total_tokens, int
  *
  * dllm_plan_pages makes the block tables of a batch hold exactly the pages its sequences need, without a host read.  Sequence
  * b needs page entry p iff it holds a position that is still read, in [0, min(keep_head, length[b])) or in [first[b],
- * length[b]) (rounded out to whole pages).  The free pages are a stack of page ids.  The call does what this order of steps
- * gives:
+ * length[b]) (rounded out to whole pages; where first[b] = length[b] inside a page, that page).  The free pages are a stack of
+ * page ids.  The call does what this order of steps gives:
  *   1. every entry >= 0 that is not needed becomes -1 and its page is pushed, sequences in order, entries ascending;
  *   2. sequence b is granted (granted[b] = 1) iff it misses no entry, or the sum of the missing entries of sequences 0 .. b
  *      is at most the number of free pages (so nobody overtakes one that waits); others keep what they have (0);
@@ -417,8 +417,8 @@ int dllm_refresh_cache(dllm_ctx *ctx, void *stream, int B, int total_tokens, int
  * dllm_slot_map lists where positions live: for the positions [start[b], end[b]) of the sequences, packed in order, slot =
  * page * page_tokens + position % page_tokens, or -1 where the table maps no page of the pool.  cu[b] = positions of the sequences
  * before b, cu[B] all of them.  slots has room for `capacity` entries (host value); those behind the last position become -1,
- * positions that do not fit are left out (DLLM_STATUS_BAD_LENGTH), as are positions outside the table (ditto).  end[b] < start[b]
- * lists nothing.
+ * positions that do not fit are left out (DLLM_STATUS_BAD_LENGTH).  start[b] and end[b] are clamped to [0, max_pages_per_seq *
+ * page_tokens] (DLLM_STATUS_BAD_LENGTH where that changes one); end[b] < start[b] lists nothing.
  *   start, end dev int32 [B]   cu dev int32 [B + 1]   slots dev int32 [capacity] */
 #define DLLM_POOL_KV  0
 #define DLLM_POOL_KV4 1

@@ -18,11 +18,12 @@ struct PlanArgs {
 struct PlanRow { int n_head, lo, hi; bool ok; };   // entries [0, n_head) and [lo, hi) are needed
 __device__ inline PlanRow plan_row(const PlanArgs& a, int b) {
   const int len = a.length[b], f = a.first ? a.first[b] : 0;
+  auto pages = [&](int n) { return n > 0 ? (n - 1) / a.pt + 1 : 0; };
   PlanRow r;
   r.ok = len >= 0 && (int64_t)len <= (int64_t)a.max_pages * a.pt && f >= 0;
-  r.n_head = r.ok ? (min(a.keep_head, len) + a.pt - 1) / a.pt : 0;
+  r.n_head = r.ok ? pages(min(a.keep_head, len)) : 0;
   r.lo = r.ok ? min(f, len) / a.pt : 0;
-  r.hi = r.ok ? (len + a.pt - 1) / a.pt : 0;
+  r.hi = r.ok ? pages(len) : 0;
   return r;
 }
 __device__ inline bool plan_needed(const PlanRow& r, int p) { return p < r.n_head || (p >= r.lo && p < r.hi); }
@@ -597,7 +598,7 @@ hipError_t launch_kv4_store(dllm_ctx* c, hipStream_t s, int n_tokens, const int3
 hipError_t launch_kv4_load(dllm_ctx* c, hipStream_t s, int n_tokens, const int32_t* src, const int32_t* dst) {
   if (c->cfg.n_layers == 0) return hipSuccess;
   const Kv4Args a = kv4_args(c, n_tokens, src, dst);
-  const dim3 grid((n_tokens + 31) / 32, c->cfg.n_kv_heads, c->cfg.n_layers);
+  const dim3 grid((n_tokens - 1) / 32 + 1, c->cfg.n_kv_heads, c->cfg.n_layers);
   if (c->cfg.head_dim == 128) k_kv4_load<128><<<grid, 256, 0, s>>>(a);
   else k_kv4_load<64><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
