@@ -416,7 +416,7 @@ hipError_t launch_s32_swiglu(dllm_ctx* c, hipStream_t s, int layer, int M, int n
 hipError_t launch_s32_logits(dllm_ctx* c, hipStream_t s, float* out, int M, int n_ss);
 hipError_t launch_s32_lmstats(dllm_ctx* c, hipStream_t s, int M, int n_ss, int* n_parts_out);
 bool attn_step_supported(const dllm_ctx* c, const StepGeom& g);
-int attn_win_parts(dllm_ctx* c, const StepGeom& g, AttnPlan* plan);
+int attn_win_parts(dllm_ctx* c, const StepGeom& g, const AttendPlan& other, AttnPlan* plan);
 hipError_t launch_attn_win(dllm_ctx* c, hipStream_t s, const StepGeom& g, const KVView& kv, const AttnPlan& p, const void* q, void* o, int out_mt);
 hipError_t launch_attn_step(dllm_ctx* c, hipStream_t s, const StepGeom& g, const KVView& kv, bool frag_out);
 

@@ -106,6 +106,40 @@ static int attn_plan_errors() {
   return errors;
 }
 
+// Attention over parts of the cache over sizes: every row has a place, the partials fit, and there are workgroups along the keys only
+// where all run at once.  Returns the number of plans that break this.
+static int attend_plan_errors() {
+  using namespace dllm;
+  int errors = 0;
+  const int heads[][2] = {{28, 4}, {32, 32}, {8, 2}, {2047, 1}};
+  for (const auto& h : heads)
+    for (int B = 1; B <= 4096; B *= 4)
+      for (int Q : {1, 2, 7, 32, 96, 1000})
+        for (int kv : {1, 33, 500, 4096, 40000, 2000000000})
+          for (int window : {0, 1, 700, 2147483647})
+            for (int four = 0; four < 2; ++four)
+              for (int bf16 = 0; bf16 < 2; ++bf16)
+                for (int64_t part_rows : {(int64_t)0, (int64_t)65536, (int64_t)1 << 40}) {
+                  if (kv < Q || (four && !bf16)) continue;
+                  const AttendPlan p = attend_plan(256, h[0], h[1], B, Q, kv, window, window, four != 0, bf16 != 0, part_rows);
+                  const int64_t wgs = (int64_t)B * h[1] * p.n_rg * p.n_parts;
+                  const bool ok = (p.qt == 1 || (p.qt == 2 && bf16)) && (int64_t)p.n_rg * 16 * p.qt >= (int64_t)Q * (h[0] / h[1]) &&
+                                  (p.kspl == 1 || p.kspl == 2 || p.kspl == 4) && p.n_parts >= 1 && p.n_parts <= ATTN_MAX_SPLITS &&
+                                  (p.n_parts == 1 || ((int64_t)p.n_parts * B * Q * h[0] <= part_rows && wgs <= 2 * 256));
+                  if (bf16 && !four) {                          // the staged kernel: page ids of a part fit, and its partials
+                    const AttnPlan w = attn_win_plan(256, 128, h[0], h[1], B, Q, kv, window, window, 64, part_rows, true, 4112, p);
+                    const int64_t span = window == 700 ? 704 + ((int64_t)700 + Q + 126) / 64 * 64 : window == 1 ? 64 + ((int64_t)Q + 127) / 64 * 64 : kv;
+                    const int64_t blocks = ((span < kv ? span : kv) + 63) / 64;
+                    if (w.staged && (w.units < 1 || w.units > ATTN_MAX_SPLITS || (w.units > 1 && (int64_t)w.units * B * Q * h[0] > part_rows) ||
+                                     (int64_t)w.pg_cap * w.units < blocks || w.lds != (size_t)DL_NB * 128 * 256 + 4 * (size_t)w.pg_cap + 4112 ||
+                                     w.lds > (size_t)DL_LDS_MAX || (int64_t)w.n_chunks * w.n_rg_wg * 32 < (int64_t)Q * (h[0] / h[1])))
+                      if (errors++ < 5) printf("staged plan over parts: heads %d/%d, B %d, Q %d, %d keys, window %d\n", h[0], h[1], B, Q, kv, window);
+                  }
+                  if (!ok && errors++ < 5) printf("plan over parts: heads %d/%d, B %d, Q %d, %d keys, window %d\n", h[0], h[1], B, Q, kv, window);
+                }
+  return errors;
+}
+
 // "form" then (kind, rows, columns, K, starts_apart) for each product: what it launches on 256 CUs, a line each.  kind "gate-up"
 // (columns: features) or "resid" (at most four K shares, one above 2048 rows): [whole rounds' column tiles +] tile [/ K shares];
 // "qkv:query heads:key heads:channels" (columns: not read): the fused kernel's tile, or "split"; "attn:query heads:key
@@ -143,6 +177,17 @@ static int print_forms(int n, char** v) {
 int main(int argc, char** argv) {
   if (argc > 1 && strcmp(argv[1], "form") == 0) return print_forms(argc - 2, argv + 2);
   EXPECT(attn_plan_errors(), 0);
+  EXPECT(attend_plan_errors(), 0);
+  // what the tests of the staged kernel over parts of the cache call: heads, channels, sequences, rows, longest prefix, window, sinks, page
+  const int staged[][9] = {{28, 4, 128, 32, 32, 200, 60, 70, 64}, {28, 4, 128, 32, 40, 300, 130, 70, 128}, {28, 4, 128, 32, 33, 200, 1, 0, 64},
+                           {28, 4, 128, 32, 20, 200, 0, 0, 64}, {28, 4, 128, 8, 32, 3000, 2000, 70, 64}, {6, 3, 64, 64, 96, 300, 100, 129, 64},
+                           {16, 1, 64, 48, 32, 600, 400, 3, 64}, {28, 4, 128, 32, 24, 100, 30, 5, 64}, {28, 4, 128, 32, 24, 190, 100, 20, 64}};
+  for (const auto& x : staged) {
+    int64_t part_rows = (int64_t)x[3] * x[4] * x[0] * 8;
+    if (part_rows < 65536) part_rows = 65536;
+    const dllm::AttendPlan other = dllm::attend_plan(256, x[0], x[1], x[3], x[4], x[5] + x[4], x[6], x[7], false, true, part_rows);
+    EXPECT(dllm::attn_win_plan(256, x[2], x[0], x[1], x[3], x[4], x[5] + x[4], x[6], x[7], x[8], part_rows, true, 16 + 32 * (size_t)x[2], other).staged, true);
+  }
   const int rings[][2] = {{2, 3}, {3, 4}, {4, 5}, {4, 6}, {3, 3}, {4, 4}};
   for (const auto& r : rings)
     for (int stages = 2; stages <= 8; ++stages)

@@ -1001,13 +1001,13 @@ hipError_t launch_attend(dllm_ctx* c, hipStream_t s, const StepGeom& g, int laye
     const int64_t part_rows = bf16 ? c->map.attn_rows : (int64_t)((c->map.rope_cos - c->map.g) / 4) / (f.head_dim + 2);
     a.part_o = bf16 ? WSM(c, attn_part, float) : WSM(c, g, float);
     a.part_ml = a.part_o + part_rows * f.head_dim;
+    const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, bf16, part_rows);
     AttnPlan staged;
-    a.n_parts = attn_win_parts(c, g, &staged);
+    a.n_parts = attn_win_parts(c, g, p, &staged);
     hipError_t e;
     if (a.n_parts > 0) {
       e = launch_attn_win(c, s, g, kv, staged, q, o, out_mt);
     } else {
-      const AttendPlan p = attend_plan(device_cus(), f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, a.window, a.n_sink, a.len4 != nullptr, bf16, part_rows);
       a.n_rg = p.n_rg; a.kspl = p.kspl; a.n_parts = p.n_parts;
       const unsigned grid = (unsigned)(((int64_t)g.B * f.n_kv_heads * p.n_parts + 7) / 8 * 8 * p.n_rg);
       const int threads = 64 * p.kspl;

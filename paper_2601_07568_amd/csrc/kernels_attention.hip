@@ -753,7 +753,7 @@ __device__ __forceinline__ void attn_dl_body(const A& a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) oacc[d][e] = 0.f;
   // (WIN: a row may read nothing of a block; from a finite maximum its weights are 0)
-  float m_run = WIN ? -1e30f : -DEV_INF, l_run = 0.f, l_odd = 0.f;
+  float m_run = WIN ? -3e38f : -DEV_INF, l_run = 0.f, l_odd = 0.f;
   const float scl = a.scale_log2;
 
   struct Wts { u32x4 hi[2], lo[2]; };                         // weights of a half: B operands of its two steps
@@ -1114,18 +1114,13 @@ hipError_t launch_attn_step(dllm_ctx* c, hipStream_t s, const StepGeom& g, const
 }
 
 // The staged kernel over what g.view lets the rows read (nothing in 4 bits), for many rows a key head: parts along the keys that it
-// left in the workspace for the caller to merge (1: the output is written), 0: not for this call.
-int attn_win_parts(dllm_ctx* c, const StepGeom& g, AttnPlan* plan) {
+// leaves in the workspace for the caller to merge (1: the output is written), 0: not for this call, which `other` is for.
+int attn_win_parts(dllm_ctx* c, const StepGeom& g, const AttendPlan& other, AttnPlan* plan) {
   const dllm_config& f = c->cfg;
   if (g.view->len4 || !attn_step_supported(c, g) || f.page_tokens % 64 != 0) return 0;   // (with small pages the registers run out)
-  // most keys of the walk, in whole blocks of 64
-  int64_t keys = g.max_kv;
-  if (g.view->window > 0) {
-    const int64_t read = ((int64_t)g.view->n_sink + 63) / 64 * 64 + ((int64_t)g.view->window + g.Q + 126) / 64 * 64;
-    if (read < keys) keys = read;
-  }
-  *plan = attn_plan(device_cus(), f.head_dim, f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.T, (int)keys, f.page_tokens, c->map.attn_rows, attn_merge_ready);
-  return plan->staged && plan->lds + dl_win_lds(f.head_dim) <= (size_t)DL_LDS_MAX ? plan->units : 0;
+  *plan = attn_win_plan(device_cus(), f.head_dim, f.n_q_heads, f.n_kv_heads, g.B, g.Q, g.max_kv, g.view->window, g.view->n_sink, f.page_tokens,
+                        c->map.attn_rows, attn_merge_ready, dl_win_lds(f.head_dim), other);
+  return plan->staged ? plan->units : 0;
 }
 hipError_t launch_attn_win(dllm_ctx* c, hipStream_t s, const StepGeom& g, const KVView& kv, const AttnPlan& p, const void* q, void* o, int out_mt) {
   const dllm_config& f = c->cfg;
@@ -1142,9 +1137,8 @@ hipError_t launch_attn_win(dllm_ctx* c, hipStream_t s, const StepGeom& g, const 
   a.status = WSM(c, status, int32_t);
   a.window = g.view->window; a.n_sink = g.view->n_sink; a.max_prefix = g.max_kv - g.Q;
   const dim3 grid(p.units, p.n_chunks, g.B * f.n_kv_heads);
-  const size_t lds = p.lds + dl_win_lds(f.head_dim);
-  if (f.head_dim == 128) k_attn_dl_win<128><<<grid, 512, lds, s>>>(a);
-  else k_attn_dl_win<64><<<grid, 512, lds, s>>>(a);
+  if (f.head_dim == 128) k_attn_dl_win<128><<<grid, 512, p.lds, s>>>(a);
+  else k_attn_dl_win<64><<<grid, 512, p.lds, s>>>(a);
   return hipGetLastError();
 }
 

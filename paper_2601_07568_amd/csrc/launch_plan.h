@@ -278,6 +278,10 @@ inline bool gt_qkv_fused(int cus, int M, int dq, int dkv, int dh, int K, int max
 }
 
 // ---- attention over parts of the cache (k_attend)
+inline int64_t attend_keys(int Q, int max_kv, int window, int n_sink) {   // most keys that the rows of a sequence read
+  const int64_t read = (int64_t)window + Q + n_sink;
+  return window > 0 && read < max_kv ? read : max_kv;
+}
 struct AttendPlan {
   int qt, n_rg;             // 16-row tiles of a wave; row groups (16 * qt rows) of a (sequence, kv head), a workgroup each
   int kspl, n_parts;        // waves of a workgroup (along the keys), workgroups along the keys
@@ -296,8 +300,7 @@ inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int
   const int rows = Q * (n_q_heads / n_kv_heads);
   p.qt = rows <= 16 || !bf16 ? 1 : 2;
   p.n_rg = (rows + 16 * p.qt - 1) / (16 * p.qt);
-  int64_t keys = max_kv;                                      // most keys that a row group reads, in blocks of its walk
-  if (window > 0 && (int64_t)window + Q + n_sink < keys) keys = (int64_t)window + Q + n_sink;
+  const int64_t keys = attend_keys(Q, max_kv, window, n_sink);
   const int64_t blocks = four ? keys / 128 + 2 : (keys + 31) / 32, per = four ? 3 : 2;
   p.kspl = blocks >= 3 ? 4 : (blocks == 2 ? 2 : 1);
   const int64_t room = (int64_t)2 * cus / ((int64_t)B * n_kv_heads * p.n_rg), want = (blocks + 4 * per - 1) / (4 * per);
@@ -305,6 +308,49 @@ inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int
   if (parts > ATTN_MAX_SPLITS) parts = ATTN_MAX_SPLITS;
   while (parts > 1 && parts * B * Q * n_q_heads > part_rows) --parts;
   p.n_parts = parts > 1 ? (int)parts : 1;
+  return p;
+}
+
+// The staged kernel (k_attn_dl_win, 512 threads and most of a CU's LDS: one workgroup a CU) over parts of the cache, or staged = false
+// where k_attend as planned in `other` (two workgroups a CU) is estimated to be quicker.  us of a round: a start and the blocks of a
+// workgroup one behind the other, 64 keys staged or four waves' 32; rows beside each other read different keys of Q / 64 blocks and
+// more, whose scores are masked one by one.  Then the parts, written and merged.  Measured / estimated, k_attend and staged with
+// 1, 2, 4, 12 parts:
+//   28/4 heads of 128, 4 x 32 rows, window 4000    44 / 44   141 / 159   83 / 93   52 / 58   35 / 39
+//   the same, 16 x 64 rows, 2048                  137 / 134   88 / 92    74 / 72   92 / 93
+//   the same, 8 x 96 rows, 500                     42 / 52    44 / 42    41 / 43   52 / 63
+//   6/3 heads of 64, 32 x 64 rows, 1000            25 / 23    33 / 35    27 / 32   33 / 43
+//   the same, 8 x 64 rows, 4000                    25 / 26    80 / 89    48 / 57   30 / 38   29 / 40
+inline AttnPlan attn_win_plan(int cus, int head_dim, int n_q_heads, int n_kv_heads, int B, int Q, int max_kv, int window, int n_sink, int page_tokens,
+                              int64_t part_rows, bool raised, size_t lds_more, const AttendPlan& other) {
+  const int64_t rows = (int64_t)B * Q * n_q_heads;
+  int64_t keys = max_kv;                                       // of the walk, in whole blocks of 64
+  if (window > 0) {
+    const int64_t read = ((int64_t)n_sink + 63) / 64 * 64 + ((int64_t)window + Q + 126) / 64 * 64;
+    if (read < keys) keys = read;
+  }
+  AttnPlan p = attn_plan(cus, head_dim, n_q_heads, n_kv_heads, B, Q, B * Q, (int)keys, page_tokens, part_rows, raised);
+  if (!p.staged) return p;
+  const int64_t blocks = (keys + 63) / 64, per_unit = (int64_t)B * n_kv_heads * p.n_chunks;
+  auto merge = [&](int64_t parts) { return parts == 1 ? 0.0 : 5.5 + (double)rows * head_dim * 8 * parts / 4.5e6; };
+  auto rounds = [](int64_t n, int64_t at_once) { return (double)((n + at_once - 1) / at_once); };
+  const double block_us = head_dim == 128 ? 2.3 : 1.2, block_other = head_dim == 128 ? 3.7 : 1.9;
+  const int64_t blocks_other = (attend_keys(Q, max_kv, window, n_sink) + 31) / 32, waves = (int64_t)other.kspl * other.n_parts;
+  const double us_other = rounds((int64_t)B * n_kv_heads * other.n_rg * other.n_parts, 2 * cus) * (2.0 + block_other * ((blocks_other + waves - 1) / waves)) +
+                          merge(other.n_parts);
+  double best = us_other;
+  p.staged = false;
+  for (int64_t u = 1; u <= blocks && u <= ATTN_MAX_SPLITS && (u == 1 || u * rows <= part_rows); ++u) {
+    const int64_t per = (blocks + u - 1) / u;
+    const size_t lds = (size_t)DL_NB * (head_dim / 4) * 1024 + 4 * (size_t)per;   // (ring, page ids: a block lies inside a page)
+    const double us = rounds(per_unit * u, cus) * (4.0 + Q / 16.0 + block_us * per) + merge(u);
+    if (us >= best || lds + lds_more > (size_t)DL_LDS_MAX) continue;
+    best = us;
+    p.staged = true;
+    p.units = (int)u;
+    p.pg_cap = (int)per;
+    p.lds = lds + lds_more;
+  }
   return p;
 }
 

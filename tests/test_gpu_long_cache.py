@@ -15,7 +15,7 @@ from tests import long_cache as R
 pytestmark = pytest.mark.gpu
 
 SMALL = synth.ModelShape(1, 64, 6, 3, 64, 64, 64, 63)                       # 2 query heads a key head
-HEADS = {"6/3x64": (6, 3, 64), "4/4x64": (4, 4, 64), "8/2x128": (8, 2, 128), "28/4x128": (28, 4, 128), "5/5x128": (5, 5, 128)}
+HEADS = {"16/1x64": (16, 1, 64), "6/3x64": (6, 3, 64), "4/4x64": (4, 4, 64), "8/2x128": (8, 2, 128), "28/4x128": (28, 4, 128), "5/5x128": (5, 5, 128)}
 
 
 def engine(heads="6/3x64", dtype="bf16", layers=1, **kw):
@@ -267,9 +267,12 @@ class Cache:
         e.attend(0, self.q.to(e.device), e.i32(self.prefix), e.i32(self.table), self.out if out is None else out, **self.kw)
         return self
 
-    def check(self, rows=None):
+    def check(self, every=1):
+        """Compares every `every`-th sequence and the last."""
         got = self.out.double().cpu().numpy()
         for b, (p, n) in enumerate(zip(self.prefix, self.valid)):
+            if b % every and b != len(self.prefix) - 1:
+                continue
             n = max(0, n)
             q = self.q[b, :n].double().numpy()
             ref, tol = R.attend(q, self.k[b], self.v[b], p, self.window, self.n_sink, self.dtype, self.n4[b])
@@ -324,6 +327,23 @@ def test_attend(i, mode):
     Cache(*CASES[i], seed=100 + i, mode=mode).run().check()
 
 
+# Calls with enough rows and sequences for the staged kernel (csrc/host_check_main.cpp holds that these get it): heads, sequences,
+# longest prefix, rows, window, sinks, page.
+STAGED = [("28/4x128", 32, 200, 32, 60, 70, 64), ("28/4x128", 32, 300, 40, 130, 70, 128), ("28/4x128", 32, 200, 33, 1, 0, 64),
+          ("28/4x128", 32, 200, 20, 0, 0, 64), ("28/4x128", 8, 3000, 32, 2000, 70, 64), ("6/3x64", 64, 300, 96, 100, 129, 64),
+          ("16/1x64", 48, 600, 32, 400, 3, 64)]
+
+
+@pytest.mark.parametrize("i", range(len(STAGED)))
+def test_attend_staged(i):
+    """Prefixes of every length up to the longest, rows that are not part of the call in some of the sequences."""
+    heads, Bn, longest, Q, window, n_sink, pt = STAGED[i]
+    rng = np.random.default_rng(300 + i)
+    prefix = [longest, 0, 63, 64] + rng.integers(0, longest + 1, Bn - 4).tolist()
+    valid = [Q, Q, 1, 0, -1] + rng.integers(0, Q + 1, Bn - 5).tolist() if i % 2 else None
+    Cache(heads, "bf16", prefix, Q, valid, None, window, n_sink, pt, seed=300 + i).run().check(every=3)
+
+
 @pytest.mark.parametrize("four", [False, True])
 @pytest.mark.parametrize("heads,Q", [("8/2x128", 1), ("8/2x128", 32), ("28/4x128", 32)])
 def test_attend_long(four, heads, Q):
@@ -336,15 +356,16 @@ def test_attend_long_float(heads, Q):
     Cache(heads, "f32", [5000, 40, 2049], Q, None, None, 0, 0, 64, seed=5 + Q, slack=700).run().check()
 
 
-@pytest.mark.parametrize("heads,pt,four,dtype", [("6/3x64", 16, False, "bf16"), ("6/3x64", 32, True, "bf16"), ("28/4x128", 64, False, "bf16"),
-                                                 ("28/4x128", 16, False, "bf16"), ("6/3x64", 20, False, "f32"), ("28/4x128", 8, False, "f32")])
+@pytest.mark.parametrize("heads,pt,four,dtype,Bn", [("6/3x64", 16, False, "bf16", 1), ("6/3x64", 32, True, "bf16", 1), ("28/4x128", 64, False, "bf16", 1),
+                                                    ("28/4x128", 64, False, "bf16", 32), ("28/4x128", 16, False, "bf16", 1),
+                                                    ("6/3x64", 20, False, "f32", 1), ("28/4x128", 8, False, "f32", 1)])
 @pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
-def test_what_is_not_read_does_not_reach_a_row(heads, pt, four, dtype, mode):
+def test_what_is_not_read_does_not_reach_a_row(heads, pt, four, dtype, Bn, mode):
     """Infinities and NaN in keys and values that some rows read and others do not: a row's output is what it would be without
     those it does not read, and not finite where it reads one."""
-    c = Cache(heads, dtype, [200], 32, None, [64] if four else None, 60, 70, pt, seed=1, mode=mode)
+    c = Cache(heads, dtype, [200] * Bn, 32, None, [64] if four else None, 60, 70, pt, seed=1, mode=mode)
     clean = c.run().out.clone()
-    c.check()
+    c.check(every=8)
     G = HEADS[heads][0] // HEADS[heads][1]
     nan, inf = float("nan"), float("inf")
     for pos, even, odd in ((150, nan, nan), (145, inf, inf), (158, -inf, None), (168, nan, inf)):   # (values of even and odd channels)
@@ -393,6 +414,26 @@ def test_scores_without_a_finite_one(mode, dtype):
     assert torch.isnan(got[0, 1:3, 5]).all() and torch.isfinite(got[0, :, 4]).all() and torch.isfinite(got[0, [0, 3], 5]).all()
 
 
+@pytest.mark.parametrize("heads,dtype,Q,pt,Bn", [("28/4x128", "bf16", 24, 64, 32), ("28/4x128", "bf16", 24, 32, 1), ("28/4x128", "f32", 24, 64, 1),
+                                                 ("5/5x128", "bf16", 3, 64, 1)])
+def test_window_without_a_finite_score(heads, dtype, Q, pt, Bn):
+    c = Cache(heads, dtype, [100] * Bn, Q, None, None, 30, 5, pt, seed=6)
+    G = HEADS[heads][0] // HEADS[heads][1]
+    c.q[..., 0] = 1.0
+    clean = c.run().out.clone()
+    k, v = c.eng.kv_slab(0, 0), c.eng.kv_slab(0, 1)
+    for pos in range(100 + Q):
+        if c.table[0, pos // pt] >= 0:
+            k[c.table[0, pos // pt], 0, pos % pt, 0] = float("-inf")
+    got = c.run().out
+    assert torch.isnan(got[0, :, :G]).all() and torch.equal(got[0, :, G:], clean[0, :, G:])
+    at = c.table[0, (99 + Q) // pt], 0, (99 + Q) % pt                        # one key is finite: the last
+    k[at] = 0.25
+    got = c.run().out
+    assert ((got[0, :, :G] - v[at]).abs() <= 4 * R.U32 * v[at].abs()).all()  # p v / p: three roundings; a bfloat16 is exact
+    assert torch.equal(got[0, :, G:], clean[0, :, G:]) and c.eng.read_status() == 0
+
+
 @pytest.mark.parametrize("mode", [0, 1], ids=["auto", "generic"])
 def test_nan_query_over_4_bits(mode):
     c = Cache("8/2x128", "bf16", [256], 4, None, [256], 0, 0, 32, seed=4, mode=mode)
@@ -415,11 +456,11 @@ def test_nan_query_over_4_bits(mode):
 def test_bad_values_on_the_device(four, dtype, heads, mode):
     """Prefix lengths beyond the host's bound and pages outside the pool are flagged; keys of such pages are left out; entries
     that map nothing that is read are not looked at."""
-    pt = 32 if four or heads == "6/3x64" else 64
-    c = Cache(heads, dtype, [190, 150], 8 if heads == "6/3x64" else 24, None, [64, 64] if four else None, 100, 20, pt, seed=8, mode=mode)
+    pt, n = (32, 1) if four or heads == "6/3x64" else (64, 16 if dtype == "bf16" else 1)
+    c = Cache(heads, dtype, [190, 150] * n, 8 if heads == "6/3x64" else 24, None, [64, 64] if four else None, 100, 20, pt, seed=8, mode=mode)
     if pt == 32:
         c.table[0, 0 if four else 1] = 12345                                # (not read: in 4 bits / between sinks and window)
-    c.run().check()
+    c.run().check(every=15)
     c.table4[1, 1], keep = -9, c.table4[1, 1]
     if four:
         c.kw["table4"] = c.eng.i32(c.table4)                                # positions 32 .. 63 of sequence 1: window starts at 51
@@ -441,7 +482,7 @@ def test_bad_values_on_the_device(four, dtype, heads, mode):
     c.table[1, 128 // pt] = keep
     for prefix, kw in (([191, 150], {}), ([-1, 150], {})):
         c.eng.reset_status()
-        c.eng.attend(0, c.q.to(c.eng.device), c.eng.i32(prefix), c.eng.i32(c.table), c.out, **{**c.kw, "max_prefix_len": 190, **kw})
+        c.eng.attend(0, c.q.to(c.eng.device), c.eng.i32(prefix + [190, 150] * (n - 1)), c.eng.i32(c.table), c.out, **{**c.kw, "max_prefix_len": 190, **kw})
         assert c.eng.read_status() & B.STATUS_BAD_LENGTH
         c.eng.reset_status()
     if four:
