@@ -385,7 +385,8 @@ hipError_t launch_slot_map(dllm_ctx* c, hipStream_t s, int n_pages, int B, int c
 // The cache in 4 bits.  One workgroup moves 32 positions of one kv head of one layer: 2 * head_dim units of 32 values that share a
 // scale (one key's 32 channels, one channel's 32 positions), four lanes a unit with 8 values (16 bytes of bfloat16, 4 of codes) each, so
 // that neighbouring lanes touch neighbouring bytes on both sides.  Bound: HBM, 4 bytes a value pair of K and V on one side and 1.06 on
-// the other.
+// the other: 8 layers of 16 sequences of 2048 positions, 4 key heads of 128, 603 MB each way: load 114 us (5.3 TB/s), store 128 .. 150 (with
+// float arithmetic for the scale and a byte store a scale 150 .. 180).
 struct Kv4Args {
   int n_tokens, pt, n_pages, n_pages4, hkv;
   char* kv;              // the pool of dllm_create
@@ -403,33 +404,54 @@ template <int DH> __device__ __forceinline__ int kv4_v_scale(int ch) { return 33
 // 2^(byte - 127), byte in 1 .. 254
 __device__ __forceinline__ float pow2_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+// largest of a value and those of the other lanes of its four
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));     // lanes 1 0 3 2
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));  // lanes 2 3 0 1
+}
 // a lane's 8 of a unit's 32 bfloat16 values -> their codes and the unit's scale byte
-__device__ __forceinline__ uint32_t kv4_quantise(const uint32_t (&x)[4], uint32_t& byte, bool& odd) {
-  uint32_t top = 0;
+__device__ __forceinline__ uint32_t kv4_quantise(uint32_t (&x)[4], uint32_t& byte, bool& odd) {
+  auto largest = [](const uint32_t (&y)[4]) -> uint32_t {       // magnitudes order like their bits
+    u16x2 m[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = x[i] & 0x7fffu, hi = (x[i] >> 16) & 0x7fffu;
-    odd |= lo >= 0x7f80u || hi >= 0x7f80u;
-    top = max(top, max(lo >= 0x7f80u ? 0u : lo, hi >= 0x7f80u ? 0u : hi));
+    for (int i = 0; i < 4; ++i) m[i] = __builtin_bit_cast(u16x2, y[i] & 0x7fff7fffu);
+    const u16x2 t = __builtin_elementwise_max(__builtin_elementwise_max(m[0], m[1]), __builtin_elementwise_max(m[2], m[3]));
+    return max((uint32_t)t[0], (uint32_t)t[1]);
+  };
+  uint32_t top = largest(x);
+  const bool wrong = top >= 0x7f80u, any = __builtin_amdgcn_ballot_w64(wrong) != 0;
+  auto part = [](uint32_t w, int i) -> uint32_t { return w >> (16 * i) & 0xffffu; };
+  if (any) {
+    uint32_t y[4];                                              // the finite values, 0 for the others
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[i] = 0;
+      for (int h = 0; h < 2; ++h) if ((part(x[i], h) & 0x7fffu) < 0x7f80u) y[i] |= x[i] & (0xffffu << (16 * h));
+    }
+    top = largest(y);
+    odd |= wrong;
   }
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+  top = quad_max(top);
   // max = (1 + m/128) 2^(e-127): 7 * 2^(e-129) holds it up to m = 96, twice that always does
   const int e = (int)(top >> 7) - 2 + ((top & 127u) > 96u ? 1 : 0);
   byte = (uint32_t)(e < 7 ? 7 : (e > 252 ? 252 : e));   // (6 * 2^125 is still a number)
   const float s = pow2_of(byte);
-  float f[8];
+  if (any) {                                            // NaN -> 0, infinity -> the largest value, 6 s
+    const uint32_t six = __float_as_uint(6.f * s) >> 16;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t b = x[i >> 1] << (i & 1 ? 0 : 16) & 0xffff0000u, m = b & 0x7fffffffu;
-    f[i] = __uint_as_float(m > 0x7f800000u ? 0u : b);                       // NaN -> 0
-    if (m == 0x7f800000u) f[i] = b >> 31 ? -6.f * s : 6.f * s;              // infinity: the largest value
+    for (int i = 0; i < 4; ++i)
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t v = part(x[i], h), m = v & 0x7fffu;
+        if (m >= 0x7f80u) x[i] = (x[i] & ~(0xffffu << (16 * h))) | (m > 0x7f80u ? 0u : (v & 0x8000u) | six) << (16 * h);
+      }
   }
   // round to nearest, ties to the even code, values beyond 6 become 6
-  uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, f[0], f[1], s, 0);
-  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[2], f[3], s, 1);
-  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[4], f[5], s, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, f[6], f[7], s, 3);
+  uint32_t v = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(bf16x2_t, x[0]), s, 0);
+  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(v, __builtin_bit_cast(bf16x2_t, x[1]), s, 1);
+  v = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(v, __builtin_bit_cast(bf16x2_t, x[2]), s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(v, __builtin_bit_cast(bf16x2_t, x[3]), s, 3);
 }
 // the values of 8 codes under a scale, as bfloat16 (exact)
 __device__ __forceinline__ uint4 kv4_values(uint32_t codes, uint32_t byte) {
@@ -446,12 +468,20 @@ __device__ __forceinline__ bool slots_run(int s, int i, int pt) {
   return s0 >= 0 && __builtin_amdgcn_ballot_w64(!(s == s0 + i && s0 % pt + i < pt)) == 0 && s0 % 8 == 0;
 }
 
+// Group of a workgroup: two that are side by side in a page, 64 bytes of V each of a 128-byte line, on one XCD (workgroups go round
+// over the eight), whose L2 then has the line for both.
+__device__ __forceinline__ int kv4_group() {
+  const int i = blockIdx.x, n = gridDim.x & ~15;
+  return i < n ? (i & ~15) + (i & 7) * 2 + ((i >> 3) & 1) : i;
+}
+
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv4_store(const Kv4Args a) {
   constexpr int NG = DH / 32, IT = DH / 32;               // 16-byte pieces of K, of V: 4 * DH each
   __shared__ int32_t s_src[32];
   __shared__ int s_ok, s_run, s_dst;
-  const int tid = threadIdx.x, grp = blockIdx.x, h = blockIdx.y, layer = blockIdx.z;
+  __shared__ uint32_t s_scale[DH / 2];                    // of K, of V: 32 * DH on in the record
+  const int tid = threadIdx.x, grp = kv4_group(), h = blockIdx.y, layer = blockIdx.z;
   const int n_slots = a.n_pages * a.pt, n_slots4 = a.n_pages4 * a.pt;       // (below 2^31, checked by the call)
   if (tid < 64) {
     const int i = tid & 31;
@@ -500,8 +530,10 @@ __global__ __launch_bounds__(256) void k_kv4_store(const Kv4Args a) {
     const int item = it * 256 + tid, u = item >> 2, part = item & 3;
     const uint32_t w = kv4_quantise(x[it], byte, odd);
     *(uint32_t*)(rec + u * 16 + part * 4) = w;            // (K and V codes: 16 bytes a unit, one behind the other)
-    if (part == 0) rec[u < DH ? kv4_k_scale<DH>(u / NG, u % NG) : kv4_v_scale<DH>(u - DH)] = (uint8_t)byte;
+    if (part == 0) ((uint8_t*)s_scale)[(u < DH ? kv4_k_scale<DH>(u / NG, u % NG) : kv4_v_scale<DH>(u - DH)) - 32 * DH] = (uint8_t)byte;
   }
+  __syncthreads();
+  if (tid < DH / 2) *(uint32_t*)(rec + 32 * DH + tid * 4) = s_scale[tid];
   if (odd) atomicOr(a.status, DLLM_STATUS_NOT_FINITE);
 }
 
@@ -511,7 +543,7 @@ __global__ __launch_bounds__(256) void k_kv4_load(const Kv4Args a) {
   __shared__ int32_t s_src[32], s_dst[32];
   __shared__ int s_run;
   const int tid = threadIdx.x, h = blockIdx.y, layer = blockIdx.z;
-  const int64_t i0 = (int64_t)blockIdx.x * 32;
+  const int64_t i0 = (int64_t)kv4_group() * 32;
   const int n_slots = a.n_pages * a.pt, n_slots4 = a.n_pages4 * a.pt;
   if (tid < 64) {
     const int i = tid & 31;
