@@ -41,7 +41,8 @@ __device__ __forceinline__ AttendSeq attend_seq(const AttendArgs& a, int b) {
 }
 
 // Any shape, both types, any page size: one workgroup per row and query head, 256 keys at a time, a thread a key for the scores and
-// a thread a channel for the sums.
+// a thread a channel for the sums.  Bound by the scores' scalar loads of K (32 sequences of 32 rows of 28/4 heads over 8192 keys in 4 bits:
+// 59 ms): for page sizes that the kernels below do not take, and to check them.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_any(const AttendArgs a, int dh) {
   __shared__ float qs[128], sc[256], red[8], part[256];
@@ -360,6 +361,12 @@ __device__ __forceinline__ void attend_finish(const AttendArgs& a, const AttendR
     }
 }
 
+// Bound, many rows: the matrix pipe (64 scaled products a block of 128 keys and 32 rows, 34 % busy) and the vector pipe beside it (58 %;
+// 16 exponentials and two conversions each of 8 values a lane and tile) at two waves a SIMD: 32 sequences of 32 rows of 28/4 heads over up to 8192 keys
+// in 4 bits 130 us in a row of calls (0.86 PFLOP/s; 152 with the running maximum followed at once and the sums by vector instructions, 137
+// before the queries went to LDS and the tiles took turns).  Few rows: reading the records (32 single tokens of 32/32 heads, windows of 4096 of
+// 32768 keys: 107 us, 5.5 TB/s).  In bfloat16: 16 KB a block of 32 keys and wave from the L2, which many row groups of a key head
+// read again and again (16 x 64 rows of 28/4 heads, windows of 2048: 137 us, the staged kernel 74).
 template <int DH, int QT>
 __global__ __launch_bounds__(256, 2) void k_attend(const AttendArgs a) {
   constexpr int KK = DH / 32, DT = DH / 16;
