@@ -361,7 +361,7 @@ __device__ __forceinline__ void attend_finish(const AttendArgs& a, const AttendR
     }
 }
 
-// Bound, many rows: the matrix pipe (64 scaled products a block of 128 keys and 32 rows, 34 % busy) and the vector pipe beside it (58 %;
+// Bound, many rows: the matrix pipe (64 scaled products a block of 128 keys and 32 rows, 42 % busy) and the vector pipe beside it (65 %;
 // 16 exponentials and two conversions each of 8 values a lane and tile) at two waves a SIMD: 32 sequences of 32 rows of 28/4 heads over up to 8192 keys
 // in 4 bits 130 us in a row of calls (0.86 PFLOP/s; 152 with the running maximum followed at once and the sums by vector instructions, 137
 // before the queries went to LDS and the tiles took turns).  Few rows: reading the records (32 single tokens of 32/32 heads, windows of 4096 of
