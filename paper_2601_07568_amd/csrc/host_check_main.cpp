@@ -181,7 +181,7 @@ int main(int argc, char** argv) {
   // what the tests of the staged kernel over parts of the cache call: heads, channels, sequences, rows, longest prefix, window, sinks, page
   const int staged[][9] = {{28, 4, 128, 32, 32, 200, 60, 70, 64}, {28, 4, 128, 32, 40, 300, 130, 70, 128}, {28, 4, 128, 32, 33, 200, 1, 0, 64},
                            {28, 4, 128, 32, 20, 200, 0, 0, 64}, {28, 4, 128, 8, 32, 3000, 2000, 70, 64}, {6, 3, 64, 64, 96, 300, 100, 129, 64},
-                           {16, 1, 64, 48, 32, 600, 400, 3, 64}, {28, 4, 128, 32, 24, 100, 30, 5, 64}, {28, 4, 128, 32, 24, 190, 100, 20, 64}};
+                           {16, 1, 64, 48, 32, 600, 400, 3, 64}, {28, 4, 128, 32, 24, 100, 30, 5, 64}, {28, 4, 128, 32, 24, 190, 100, 20, 64}, {28, 4, 128, 32, 32, 200, 2147483647, 2147483647, 64}};
   for (const auto& x : staged) {
     int64_t part_rows = (int64_t)x[3] * x[4] * x[0] * 8;
     if (part_rows < 65536) part_rows = 65536;

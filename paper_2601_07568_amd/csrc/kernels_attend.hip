@@ -269,7 +269,7 @@ __device__ __forceinline__ AttendRows attend_rows(const AttendArgs& a) {
 // row (token * Hq + head) of the lane's query in tile t (of the last one beyond the end), and the position above which it reads keys
 __device__ __forceinline__ int attend_row(const AttendArgs& a, const AttendRows& v, int r, int& wlo) {
   const int rr = min(r, v.R - 1), hg = rr / v.sq.n_q, j = rr - hg * v.sq.n_q;
-  wlo = a.window > 0 ? v.sq.pl + j - a.window : -1;
+  wlo = a.window > 0 ? max(-1, v.sq.pl + j - a.window) : -1;   // (differences with keys stay in 32 bits)
   return (v.b * a.Q + j) * a.Hq + v.kvh * (a.Hq / a.Hkv) + hg;
 }
 __device__ __forceinline__ void attend_report(const AttendArgs& a, const AttendRows& v, bool bad) {

@@ -679,7 +679,7 @@ __device__ __forceinline__ void attn_dl_body(const A& a) {
     const int hg = rr / n_q, j = rr - hg * n_q;
     const int64_t ro = (int64_t)(row_base + j) * a.Hq + kvh * G + hg;
     row_out = ok ? ro : -1;
-    if constexpr (WIN) wlo = a.window > 0 ? pl + j - a.window : -1;
+    if constexpr (WIN) wlo = a.window > 0 ? max(-1, pl + j - a.window) : -1;
     const bf16_t* qp = a.q + ro * DH + h * 8;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) qf[kk] = *(const u32x4*)(qp + kk * 16);

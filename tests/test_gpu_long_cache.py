@@ -219,7 +219,7 @@ class Cache:
         self.max_prefix = max(prefix) + slack
         eng.set_kernel_mode(mode)
         dt = torch.bfloat16 if dtype == "bf16" else torch.float32
-        self.prefix, self.valid = prefix, [Q] * Bn if valid is None else valid
+        self.prefix, self.valid = prefix, [Q] * Bn if valid is None else [min(n, Q) for n in valid]
         self.n4 = [min(f, p) // 32 * 32 for f, p in zip(four, prefix)] if four else [0] * Bn
         self.q = torch.tensor(rng.standard_normal((Bn, Q, hq, dh))).to(dt)
         perm = rng.permutation(Bn * NP)
@@ -318,6 +318,9 @@ CASES = [
     ("6/3x64", "f32", [900, 17], 40, [40, -1], None, 0, 0, 4),
     ("5/5x128", "f32", [2000], 3, None, None, 1999, 1, 20),
     ("6/3x64", "f32", [64, 31], 2, None, None, 1, 0, 32),
+    ("8/2x128", "bf16", [100, 3], 5, [2 ** 31 - 1, 3], None, 2 ** 31 - 1, 0, 32),
+    ("28/4x128", "bf16", [100, 300], 33, [33, 99], [96, 288], 2 ** 31 - 1, 2 ** 31 - 1, 32),
+    ("6/3x64", "f32", [100, 3], 5, None, None, 2 ** 31 - 1, 7, 32),
 ]
 
 
@@ -331,7 +334,7 @@ def test_attend(i, mode):
 # longest prefix, rows, window, sinks, page.
 STAGED = [("28/4x128", 32, 200, 32, 60, 70, 64), ("28/4x128", 32, 300, 40, 130, 70, 128), ("28/4x128", 32, 200, 33, 1, 0, 64),
           ("28/4x128", 32, 200, 20, 0, 0, 64), ("28/4x128", 8, 3000, 32, 2000, 70, 64), ("6/3x64", 64, 300, 96, 100, 129, 64),
-          ("16/1x64", 48, 600, 32, 400, 3, 64)]
+          ("16/1x64", 48, 600, 32, 400, 3, 64), ("28/4x128", 32, 200, 32, 2 ** 31 - 1, 2 ** 31 - 1, 64)]
 
 
 @pytest.mark.parametrize("i", range(len(STAGED)))
