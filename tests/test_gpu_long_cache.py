@@ -567,7 +567,8 @@ def test_streams_and_replays():
     def fresh():
         return dict(t=eng.i32([[-1] * 12] * 3), s=eng.i32(list(range(64))[::-1]), n=eng.i32([64]), t4=eng.i32([[-1] * 12] * 3),
                     s4=eng.i32(list(range(40))), n4=eng.i32([40]), cu=eng.i32([0] * 4), a=eng.i32([0] * 448), d=eng.i32([0] * 448),
-                    out=torch.zeros_like(q))
+                    out=torch.zeros_like(q), cand=eng.i32([[0] * 4] * 3), conf=torch.zeros(3, 4, device=eng.device))
+    toks = eng.i32([[eng.ms.mask_id, 1, 2, eng.ms.mask_id]] * 3)
 
     def turn(x):
         eng.plan_pages(total, x["t"], x["s"], x["n"])
@@ -575,6 +576,7 @@ def test_streams_and_replays():
         eng.slot_map(zero, len4, x["t"], x["cu"], x["a"])
         eng.slot_map(zero, len4, x["t4"], x["cu"], x["d"], kv4=True)
         eng.kv4_store(x["a"], x["d"])
+        eng.denoise_step_view(toks, length, x["t"], x["cand"], x["conf"], max_prefix_len=300, len4=len4, table4=x["t4"], window=200, n_sink=40)
         eng.attend(0, q, length, x["t"], x["out"], max_prefix_len=300, len4=len4, table4=x["t4"], window=200, n_sink=40)
     eager = fresh()
     turn(eager)
@@ -693,3 +695,29 @@ def test_turn_of_a_long_sequence(dtype, Q, valid, mode):
             r = {"logits": logits, "cand": O.confidence(logits, 511)[0]}
             H.check_step_outputs(ms, r, masked, cand[b, :n].cpu().numpy(), conf[b, :n].cpu().numpy(), ent[b, :n].cpu().numpy(), dtype)
             assert (cand[b].cpu().numpy()[n:] == block[b, n:]).all() and (conf[b, n:] == 1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_step_of_many_rows_over_a_window(dtype):
+    """A batch whose steps take the tiled products and the staged attention (bfloat16), rows that are not part of the step in some."""
+    ms = dataclasses.replace(SMALL, n_layers=1, d_model=256, n_q_heads=28, n_kv_heads=4, head_dim=128, d_ff=128, vocab=512, mask_id=511, dtype=dtype,
+                             lm_head_scale=8.0)
+    w = synth.Weights(ms, 5)
+    Bn, Q, prompt = 32, 32, 200
+    eng = H.make_engine(ms, w, page_tokens=64, max_pages_per_seq=4, n_pages=4 * Bn, max_batch=Bn, max_q=Q, max_tokens=Bn * prompt)
+    rng = np.random.default_rng(12)
+    table = rng.permutation(4 * Bn).reshape(Bn, 4)
+    bt, pl = eng.i32(table), eng.i32([prompt] * Bn)
+    eng.prefill_kv(eng.i32(rng.integers(0, 511, Bn * prompt)), eng.i32(np.arange(Bn + 1) * prompt), bt, total_tokens=Bn * prompt, max_seqlen=prompt)
+    block = np.where(rng.random((Bn, Q)) < 0.7, 511, rng.integers(0, 511, (Bn, Q))).astype(np.int32)
+    valid = [Q, 7, 0] + [Q] * (Bn - 4) + [31]
+    cand = torch.zeros(Bn, Q, dtype=torch.int32, device=eng.device)
+    conf, ent = torch.zeros(Bn, Q, device=eng.device), torch.zeros(Bn, Q, device=eng.device)
+    eng.denoise_step_view(eng.i32(block), pl, bt, cand, conf, ent, max_prefix_len=prompt, q_valid=eng.i32(valid), window=60, n_sink=70)
+    assert eng.read_status() == 0
+    for b in (0, 1, 16, Bn - 1):
+        n = valid[b]
+        cache = [[H.gather_cache(eng, table[b], prompt, 0, x).astype(np.float64) for x in (0, 1)]]
+        logits = view_step(ms, w, block[b], cache, prompt, 60, 70, n, synth.as_float if dtype == "bf16" else None, H.STORE[dtype])
+        H.check_step_outputs(ms, {"logits": logits, "cand": O.confidence(logits, 511)[0]}, block[b, :n] == 511, cand[b, :n].cpu().numpy(),
+                             conf[b, :n].cpu().numpy(), ent[b, :n].cpu().numpy(), dtype)
