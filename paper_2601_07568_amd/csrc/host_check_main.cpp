@@ -125,7 +125,7 @@ static int attend_plan_errors() {
                   const int64_t wgs = (int64_t)B * h[1] * p.n_rg * p.n_parts;
                   const bool ok = (p.qt == 1 || (p.qt == 2 && bf16)) && (int64_t)p.n_rg * 16 * p.qt >= (int64_t)Q * (h[0] / h[1]) &&
                                   (p.kspl == 1 || p.kspl == 2 || p.kspl == 4) && p.n_parts >= 1 && p.n_parts <= ATTN_MAX_SPLITS &&
-                                  (p.n_parts == 1 || ((int64_t)p.n_parts * B * Q * h[0] <= part_rows && wgs <= 2 * 256));
+                                  (p.n_parts == 1 || ((int64_t)p.n_parts * B * Q * h[0] <= part_rows && wgs <= (four ? 512 : 256)));
                   if (bf16 && !four) {                          // the staged kernel: page ids of a part fit, and its partials
                     const AttnPlan w = attn_win_plan(256, 128, h[0], h[1], B, Q, kv, window, window, 64, part_rows, true, 4112, p);
                     const int64_t span = window == 700 ? 704 + ((int64_t)700 + Q + 126) / 64 * 64 : window == 1 ? 64 + ((int64_t)Q + 127) / 64 * 64 : kv;
@@ -181,7 +181,7 @@ int main(int argc, char** argv) {
   // what the tests of the staged kernel over parts of the cache call: heads, channels, sequences, rows, longest prefix, window, sinks, page
   const int staged[][9] = {{28, 4, 128, 32, 32, 200, 60, 70, 64}, {28, 4, 128, 32, 40, 300, 130, 70, 128}, {28, 4, 128, 32, 33, 200, 1, 0, 64},
                            {28, 4, 128, 32, 20, 200, 0, 0, 64}, {28, 4, 128, 8, 32, 3000, 2000, 70, 64}, {6, 3, 64, 64, 96, 300, 100, 129, 64},
-                           {16, 1, 64, 48, 32, 600, 400, 3, 64}, {28, 4, 128, 32, 24, 100, 30, 5, 64}, {28, 4, 128, 32, 24, 190, 100, 20, 64}, {28, 4, 128, 32, 32, 200, 2147483647, 2147483647, 64}};
+                           {6, 3, 64, 16, 96, 2100, 2000, 3, 64}, {28, 4, 128, 32, 24, 100, 30, 5, 64}, {28, 4, 128, 32, 24, 190, 100, 20, 64}, {28, 4, 128, 32, 32, 200, 2147483647, 2147483647, 64}};
   for (const auto& x : staged) {
     int64_t part_rows = (int64_t)x[3] * x[4] * x[0] * 8;
     if (part_rows < 65536) part_rows = 65536;

@@ -293,8 +293,12 @@ struct AttendPlan {
 //   32 row groups, 1072 of bfloat16                     1x4x1 23.5   1x4x3 17.4   1x4x6 17.4   4x1x6 18.9
 //   512 row groups, up to 4160 in 4 bits                1x4x1 51.8   1x4x2 62.1   2x2x1 56.9   4x1x2 81.5
 //   896 row groups, up to 8224 in 4 bits                1x4x1 140    1x4x2 148    2x2x1 142    4x1x2 150
-// so: one row group a workgroup, parts along the keys only where a round of two workgroups a CU has room for them and a wave of
-// one workgroup would have more than three blocks of 128 keys or two of 32 (merging the parts is a launch: 2.5 us and more).
+// so: one row group a workgroup, parts along the keys only where each of them has a CU of its own and a wave of one workgroup would
+// have more than three blocks of 128 keys or two of 32 (merging the parts is a launch: 2.5 us and more), and no more than it takes for a
+// wave to have as few blocks.  Up to two workgroups a CU / one: 32/32 heads, 32 rows, windows of 2048 24.0 / 18.5, of 4096 28.2 / 24.4, 16000 keys in 4
+// bits 28.6 / 23.9; 28/4 heads, 32 rows, window 4096 26.2 / 21.6, 4 sequences, window 1000 26.6 / 21.3, 16000 keys in 4 bits 25.6 / 21.6.  Keys in 4 bits
+// wait for their arithmetic, so two where one leaves a quarter of the CUs without: 6/3 heads, 8 sequences of 96 rows and 8000 keys 30.9 /
+// 39.4; 28/4 heads, 96 rows, 8000 keys 27.0 / 31.0.
 inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int Q, int max_kv, int window, int n_sink, bool four, bool bf16, int64_t part_rows) {
   AttendPlan p{};
   const int rows = Q * (n_q_heads / n_kv_heads);
@@ -303,24 +307,32 @@ inline AttendPlan attend_plan(int cus, int n_q_heads, int n_kv_heads, int B, int
   const int64_t keys = attend_keys(Q, max_kv, window, n_sink);
   const int64_t blocks = four ? keys / 128 + 2 : (keys + 31) / 32, per = four ? 3 : 2;
   p.kspl = blocks >= 3 ? 4 : (blocks == 2 ? 2 : 1);
-  const int64_t room = (int64_t)2 * cus / ((int64_t)B * n_kv_heads * p.n_rg), want = (blocks + 4 * per - 1) / (4 * per);
+  // (an XCD has an eighth of the CUs and the row groups of a part one behind the other)
+  const int64_t seqs = (int64_t)B * n_kv_heads, want = (blocks + 4 * per - 1) / (4 * per);
+  auto room_of = [&](int at_once) { return (at_once / 8 >= p.n_rg ? (int64_t)(at_once / 8 / p.n_rg) * 8 : (int64_t)at_once / p.n_rg) / seqs; };
+  int64_t room = room_of(cus);
+  if (four && room < want && room * seqs * p.n_rg * 4 < (int64_t)3 * cus) room = room_of(2 * cus);
   int64_t parts = room < want ? room : want;
   if (parts > ATTN_MAX_SPLITS) parts = ATTN_MAX_SPLITS;
   while (parts > 1 && parts * B * Q * n_q_heads > part_rows) --parts;
+  if (parts > 1) {                                            // no more than it takes for a wave to have as few blocks
+    const int64_t wave = (blocks + 4 * parts - 1) / (4 * parts);
+    parts = (blocks + 4 * wave - 1) / (4 * wave);
+  }
   p.n_parts = parts > 1 ? (int)parts : 1;
   return p;
 }
 
 // The staged kernel (k_attn_dl_win, 512 threads and most of a CU's LDS: one workgroup a CU) over parts of the cache, or staged = false
 // where k_attend as planned in `other` (two workgroups a CU) is estimated to be quicker.  us of a round: a start and the blocks of a
-// workgroup one behind the other, 64 keys staged or four waves' 32; rows beside each other read different keys of Q / 64 blocks and
-// more, whose scores are masked one by one.  Then the parts, written and merged.  Measured / estimated, k_attend and staged with
-// 1, 2, 4, 12 parts:
-//   28/4 heads of 128, 4 x 32 rows, window 4000    44 / 44   141 / 159   83 / 93   52 / 58   35 / 39
-//   the same, 16 x 64 rows, 2048                  137 / 134   88 / 92    74 / 72   92 / 93
-//   the same, 8 x 96 rows, 500                     42 / 52    44 / 42    41 / 43   52 / 63
-//   6/3 heads of 64, 32 x 64 rows, 1000            25 / 23    33 / 35    27 / 32   33 / 43
-//   the same, 8 x 64 rows, 4000                    25 / 26    80 / 89    48 / 57   30 / 38   29 / 40
+// workgroup one behind the other, 64 keys staged (few row groups keep half of the waves free) or four waves' 32, which a second
+// workgroup on the CU slows down; rows beside each other read different keys of Q / 64 blocks and more, whose scores are masked one
+// by one.  Then the parts, written and merged.  k_attend / staged, measured (estimated; the least of a launch apart):
+//   28/4 heads of 128, 4 x 32 rows, window 4000    41 / 34 (39 / 33)      the same, 4 x 64 rows, 1000     25 / 31 (22 / 29)
+//   the same, 16 x 64 rows, 2048                  135 / 73 (135 / 72)     32 x 32 rows, 500               52 / 42 (47 / 37)
+//   the same, 8 x 96 rows, 500                     42 / 47 (38 / 38)      2 x 32 rows, 4000               26 / 29 (23 / 26)
+//   6/3 heads of 64, 32 x 64 rows, 1000            25 / 27 (20 / 24)      32 x 96 rows, 300               23 / 29 (20 / 24)
+//   the same, 16 x 96 rows, 2000                   38 / 28 (33 / 28)      8 x 64 rows, 4000               30 / 23 (23 / 22)
 inline AttnPlan attn_win_plan(int cus, int head_dim, int n_q_heads, int n_kv_heads, int B, int Q, int max_kv, int window, int n_sink, int page_tokens,
                               int64_t part_rows, bool raised, size_t lds_more, const AttendPlan& other) {
   const int64_t rows = (int64_t)B * Q * n_q_heads;
@@ -332,18 +344,19 @@ inline AttnPlan attn_win_plan(int cus, int head_dim, int n_q_heads, int n_kv_hea
   AttnPlan p = attn_plan(cus, head_dim, n_q_heads, n_kv_heads, B, Q, B * Q, (int)keys, page_tokens, part_rows, raised);
   if (!p.staged) return p;
   const int64_t blocks = (keys + 63) / 64, per_unit = (int64_t)B * n_kv_heads * p.n_chunks;
-  auto merge = [&](int64_t parts) { return parts == 1 ? 0.0 : 5.5 + (double)rows * head_dim * 8 * parts / 4.5e6; };
-  auto rounds = [](int64_t n, int64_t at_once) { return (double)((n + at_once - 1) / at_once); };
-  const double block_us = head_dim == 128 ? 2.3 : 1.2, block_other = head_dim == 128 ? 3.7 : 1.9;
-  const int64_t blocks_other = (attend_keys(Q, max_kv, window, n_sink) + 31) / 32, waves = (int64_t)other.kspl * other.n_parts;
-  const double us_other = rounds((int64_t)B * n_kv_heads * other.n_rg * other.n_parts, 2 * cus) * (2.0 + block_other * ((blocks_other + waves - 1) / waves)) +
-                          merge(other.n_parts);
+  const bool wide = head_dim == 128;
+  auto merge = [&](int64_t parts) { return parts == 1 ? 0.0 : 2.2 + (double)rows * head_dim * 8 * parts / 5.2e6; };
+  const double block_us = (wide ? 2.8 : 1.6) * (p.n_rg_wg > 4 ? 1.0 : 0.75);
+  const int64_t waves = (int64_t)other.kspl * other.n_parts, wgs = (int64_t)B * n_kv_heads * other.n_rg * other.n_parts, last = wgs % (2 * cus);
+  const int64_t other_blocks = ((attend_keys(Q, max_kv, window, n_sink) + 31) / 32 + waves - 1) / waves;
+  const double us_two = 4.8 + (wide ? 3.7 : 1.65) * other_blocks, us_one = 4.8 + (wide ? 1.9 : 1.0) * other_blocks;
+  const double us_other = wgs / (2 * cus) * us_two + (last == 0 ? 0.0 : last <= cus ? us_one : us_two) + merge(other.n_parts);
   double best = us_other;
   p.staged = false;
   for (int64_t u = 1; u <= blocks && u <= ATTN_MAX_SPLITS && (u == 1 || u * rows <= part_rows); ++u) {
     const int64_t per = (blocks + u - 1) / u;
     const size_t lds = (size_t)DL_NB * (head_dim / 4) * 1024 + 4 * (size_t)per;   // (ring, page ids: a block lies inside a page)
-    const double us = rounds(per_unit * u, cus) * (4.0 + Q / 16.0 + block_us * per) + merge(u);
+    const double us = (per_unit * u + cus - 1) / cus * (5.7 + Q / 20.0 + block_us * per) + merge(u);
     if (us >= best || lds + lds_more > (size_t)DL_LDS_MAX) continue;
     best = us;
     p.staged = true;
