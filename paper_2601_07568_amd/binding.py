@@ -167,7 +167,7 @@ class Engine:
         self.workspace = torch.empty(ws_bytes + 256, dtype=torch.uint8, device=self.device)
         self._ws_off = (-self.workspace.data_ptr()) % 256
         self.kv_pool = torch.zeros(max(kv_bytes, 1), dtype=torch.uint8, device=self.device)
-        self._lib, self._home = L, self.kv_pool.device
+        self._lib, self._home, self._row = L, self.kv_pool.device, self.cfg.max_pages_per_seq
         self._kv_typed = self.kv_pool.view(self.tdtype) if kv_bytes else None
         self.ctx = C.c_void_p()
         rc = L.dllm_create(C.byref(self.ctx), C.byref(self.cfg), C.byref(self._w), self.kv_pool.data_ptr(),
@@ -357,13 +357,17 @@ class Engine:
 
     # -- long caches
     def _dev(self, name, t, dtype, shape):
-        """Address of a contiguous tensor of this device; the calls below check what the library cannot see.  None: NULL."""
-        if t is None:
-            return None
-        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != self._home:
-            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {list(shape)} on {self._home}, got {t.dtype} "
-                             f"{list(t.shape)} with strides {list(t.stride())} on {t.device}")
-        return t.data_ptr()
+        """Address of a contiguous tensor of this device; the calls below check what the library cannot see."""
+        try:
+            if t.dtype is dtype and t.shape == shape and t.get_device() == self._home.index and t.is_contiguous():
+                return t.data_ptr()
+        except AttributeError:
+            raise ValueError(f"{name}: a tensor is needed, got {t!r}") from None
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {list(shape)} on {self._home}, got {t.dtype} "
+                         f"{list(t.shape)} with strides {list(t.stride())} on {t.device}")
+
+    def _opt(self, name, t, dtype, shape):
+        return None if t is None else self._dev(name, t, dtype, shape)
 
     def _call(self, fn, *args):
         """One library call on the current stream of the engine's device, with that device current."""
@@ -396,59 +400,49 @@ class Engine:
         return (POOL_KV4, self.n_pages4) if kv4 else (POOL_KV, self.cfg.n_pages)
 
     def plan_pages(self, length, block_table, free_pages, n_free, granted=None, *, first=None, keep_head=0, kv4=False):
-        i32, (pool, n_pages), B, dev = self.torch.int32, self._pool(kv4), length.numel(), self._dev
-        self._need(length=length, block_table=block_table, free_pages=free_pages, n_free=n_free)
-        self._call(self._lib.dllm_plan_pages, pool, B, keep_head, dev("length", length, i32, (B,)), dev("first", first, i32, (B,)),
-                   dev("block_table", block_table, i32, (B, self.cfg.max_pages_per_seq)), dev("free_pages", free_pages, i32, (n_pages,)),
-                   dev("n_free", n_free, i32, (1,)), dev("granted", granted, i32, (B,)))
+        i32, (pool, n_pages), B, dev, opt = self.torch.int32, self._pool(kv4), length.numel(), self._dev, self._opt
+        self._call(self._lib.dllm_plan_pages, pool, B, keep_head, dev("length", length, i32, (B,)), opt("first", first, i32, (B,)),
+                   dev("block_table", block_table, i32, (B, self._row)), dev("free_pages", free_pages, i32, (n_pages,)),
+                   dev("n_free", n_free, i32, (1,)), opt("granted", granted, i32, (B,)))
 
     def slot_map(self, start, end, block_table, cu, slots, *, kv4=False):
-        i32, pool, B, dev = self.torch.int32, self._pool(kv4)[0], start.numel(), self._dev
-        self._need(end=end, block_table=block_table, cu=cu, slots=slots)
-        n = slots.numel()
+        i32, pool, B, n, dev = self.torch.int32, self._pool(kv4)[0], start.numel(), slots.numel(), self._dev
         self._call(self._lib.dllm_slot_map, pool, B, n, dev("start", start, i32, (B,)), dev("end", end, i32, (B,)),
-                   dev("block_table", block_table, i32, (B, self.cfg.max_pages_per_seq)), dev("cu", cu, i32, (B + 1,)),
-                   dev("slots", slots, i32, (n,)))
+                   dev("block_table", block_table, i32, (B, self._row)), dev("cu", cu, i32, (B + 1,)), dev("slots", slots, i32, (n,)))
 
     def kv4_store(self, src_slots, dst_slots):
         i32, n = self.torch.int32, src_slots.numel()
-        self._need(dst_slots=dst_slots)
         self._call(self._lib.dllm_kv4_store, n, self._dev("src_slots", src_slots, i32, (n,)), self._dev("dst_slots", dst_slots, i32, (n,)))
 
     def kv4_load(self, src_slots, dst_slots):
         i32, n = self.torch.int32, src_slots.numel()
-        self._need(dst_slots=dst_slots)
         self._call(self._lib.dllm_kv4_load, n, self._dev("src_slots", src_slots, i32, (n,)), self._dev("dst_slots", dst_slots, i32, (n,)))
 
-    def _need(self, **tensors):
-        for name, t in tensors.items():
-            if t is None:
-                raise ValueError(f"{name}: a tensor is needed")
-
     def _view(self, B, window, n_sink, len4, table4):
+        """The record of what is read (None: everything, nothing in 4 bits)."""
+        if len4 is None and table4 is None:
+            return None if window == 0 and n_sink >= 0 else C.byref(CacheView(window, n_sink, None, None))
         i32 = self.torch.int32
-        return C.byref(CacheView(window, n_sink, self._dev("len4", len4, i32, (B,)),
-                                 self._dev("table4", table4, i32, (B, self.cfg.max_pages_per_seq))))
+        return C.byref(CacheView(window, n_sink, self._opt("len4", len4, i32, (B,)), self._opt("table4", table4, i32, (B, self._row))))
 
     def attend(self, layer, q, prefix_len, block_table, out, *, max_prefix_len, q_valid=None, window=0, n_sink=0, len4=None,
                table4=None):
-        i32, dev, cfg, (B, Q) = self.torch.int32, self._dev, self.cfg, q.shape[:2]
-        self._need(prefix_len=prefix_len, block_table=block_table, out=out)
+        i32, dev, cfg = self.torch.int32, self._dev, self.cfg
+        B, Q = q.shape[:2]
         shape = (B, Q, cfg.n_q_heads, cfg.head_dim)
         self._call(self._lib.dllm_attend, layer, B, Q, max_prefix_len, dev("q", q, self.tdtype, shape),
-                   dev("prefix_len", prefix_len, i32, (B,)), dev("q_valid", q_valid, i32, (B,)),
-                   dev("block_table", block_table, i32, (B, cfg.max_pages_per_seq)),
+                   dev("prefix_len", prefix_len, i32, (B,)), self._opt("q_valid", q_valid, i32, (B,)),
+                   dev("block_table", block_table, i32, (B, self._row)),
                    self._view(B, window, n_sink, len4, table4), dev("out", out, self.tdtype, shape))
 
     def denoise_step_view(self, q_tokens, prefix_len, block_table, cand, conf, entropy=None, *, max_prefix_len, q_valid=None,
                           window=0, n_sink=0, len4=None, table4=None):
-        i32, f32, dev, (B, Q) = self.torch.int32, self.torch.float32, self._dev, q_tokens.shape
-        self._need(prefix_len=prefix_len, block_table=block_table, cand=cand, conf=conf)
+        i32, f32, dev, opt, (B, Q) = self.torch.int32, self.torch.float32, self._dev, self._opt, q_tokens.shape
         self._call(self._lib.dllm_denoise_step_view, B, Q, max_prefix_len, dev("q_tokens", q_tokens, i32, (B, Q)),
-                   dev("prefix_len", prefix_len, i32, (B,)), dev("q_valid", q_valid, i32, (B,)),
-                   dev("block_table", block_table, i32, (B, self.cfg.max_pages_per_seq)),
+                   dev("prefix_len", prefix_len, i32, (B,)), opt("q_valid", q_valid, i32, (B,)),
+                   dev("block_table", block_table, i32, (B, self._row)),
                    self._view(B, window, n_sink, len4, table4), dev("cand", cand, i32, (B, Q)),
-                   dev("conf", conf, f32, (B, Q)), dev("entropy", entropy, f32, (B, Q)))
+                   dev("conf", conf, f32, (B, Q)), opt("entropy", entropy, f32, (B, Q)))
 
     def debug_logits(self, q_tokens, prefix_len, block_table, *, max_prefix_len):
         B, Q = q_tokens.shape
