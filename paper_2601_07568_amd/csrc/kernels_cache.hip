@@ -98,14 +98,12 @@ __device__ inline int plan_top(const PlanArgs& a, int nf, int64_t rel, bool repo
 __device__ inline int plan_grant(int need, int64_t before, int top) {
   return need < 0 ? -1 : (need == 0 ? 0 : (before + need <= top ? (int)before : -1));
 }
-// One wave: what sequence b gives back goes onto the stack.
-__device__ inline void plan_release(const PlanArgs& a, int b, int lane, int at) {
-  const PlanRow r = plan_row(a, b);
+// One wave: what sequence b gives back goes onto the stack.  e: the first entries of the row.
+__device__ inline void plan_release(const PlanArgs& a, const PlanRow& r, int b, int lane, int at, int32_t (&e)[PLAN_ROW / 64]) {
   if (!r.ok) return;
   bool bad = false;
   for (int p0 = 0; p0 < a.max_pages; p0 += PLAN_ROW) {
-    int32_t e[PLAN_ROW / 64];
-    plan_row_entries(a, b, p0, lane, a.max_pages, e);
+    if (p0 > 0) plan_row_entries(a, b, p0, lane, a.max_pages, e);
 #pragma unroll
     for (int i = 0; i < PLAN_ROW / 64; ++i) {
       const int p = p0 + i * 64 + lane;
@@ -121,13 +119,12 @@ __device__ inline void plan_release(const PlanArgs& a, int b, int lane, int at) 
   }
   if (bad) atomicOr(a.status, DLLM_STATUS_BAD_PAGE);
 }
-// One wave: the missing entries of sequence b pop their pages, from place `at` on downwards.
-__device__ inline void plan_take(const PlanArgs& a, int b, int lane, int at) {
-  const PlanRow r = plan_row(a, b);
+// One wave: the missing entries of sequence b pop their pages, from place `at` on downwards.  e: the first entries of the row.
+__device__ inline void plan_take(const PlanArgs& a, const PlanRow& r, int b, int lane, int at, int32_t (&e)[PLAN_ROW / 64]) {
   bool bad = false;
   for (int p0 = 0; p0 < r.hi; p0 += PLAN_ROW) {           // (no needed entry behind hi: n_head <= hi)
-    int32_t e[PLAN_ROW / 64], page[PLAN_ROW / 64];
-    plan_row_entries(a, b, p0, lane, a.max_pages, e);
+    int32_t page[PLAN_ROW / 64];
+    if (p0 > 0) plan_row_entries(a, b, p0, lane, a.max_pages, e);
     uint32_t miss = 0;
 #pragma unroll
     for (int i = 0; i < PLAN_ROW / 64; ++i) {
@@ -185,9 +182,17 @@ __global__ __launch_bounds__(1024) void k_plan_one(const PlanArgs a) {
     if (lane == 0) a.n_free[0] = left;
   }
   __syncthreads();
-  if (w < a.B && s_rel[w] != 0) plan_release(l, w, lane, s_push[w]);
+  if (w < a.B && s_rel[w] != 0) {
+    int32_t e[PLAN_ROW / 64];
+    plan_row_entries(l, w, 0, lane, a.max_pages, e);
+    plan_release(l, plan_row(l, w), w, lane, s_push[w], e);
+  }
   __syncthreads();
-  if (w < a.B && s_pop[w] >= 0) plan_take(l, w, lane, s_pop[w]);
+  if (w < a.B && s_pop[w] >= 0) {
+    int32_t e[PLAN_ROW / 64];
+    plan_row_entries(l, w, 0, lane, a.max_pages, e);
+    plan_take(l, plan_row(l, w), w, lane, s_pop[w], e);
+  }
 }
 
 // Large batches.  Every workgroup adds up by itself what the sequences before its four give back (miss).
@@ -212,28 +217,39 @@ __global__ __launch_bounds__(256) void k_plan_release(const PlanArgs a) {
   __shared__ int64_t sm[4];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, b0 = blockIdx.x * 4, b = b0 + w;
   const int nf = a.hdr[0];
+  const int row = min(b, a.B - 1), rel = a.rel[row];           // (as in k_plan_take)
+  const PlanRow r = plan_row(a, row);
+  int32_t e[PLAN_ROW / 64];
+  plan_row_entries(a, row, 0, lane, a.max_pages, e);
   int64_t total;
   auto given = [&](int i) { return plan_given(a.rel[i]); };
   int64_t before = plan_sum(given, b0, a.B, sm, total);
   if (blockIdx.x == 0 && threadIdx.x == 0) a.n_free[0] = a.hdr[1] = plan_top(a, nf, total, true);   // plan_take lowers it to what is left
-  if (b >= a.B || a.rel[b] == 0) return;
+  if (b >= a.B || rel == 0) return;
   for (int i = b0; i < b; ++i) before += given(i);
-  plan_release(a, b, lane, (int)min((int64_t)a.n_pages, nf + before));
+  plan_release(a, r, b, lane, (int)min((int64_t)a.n_pages, nf + before), e);
 }
 __global__ __launch_bounds__(256) void k_plan_take(const PlanArgs a) {
   __shared__ int64_t sm[4];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, b0 = blockIdx.x * 4, b = b0 + w;
   const int top = a.hdr[1];
+  // (the row travels while the sums are made)
+  const int row = min(b, a.B - 1), need = a.need[row];
+  const PlanRow r = plan_row(a, row);
+  int32_t e[PLAN_ROW / 64];
+  plan_row_entries(a, row, 0, lane, a.max_pages, e);
   int64_t total;
   auto missing = [&](int i) { return max(a.need[i], 0); };
   int64_t before = plan_sum(missing, b0, a.B, sm, total);
+  const bool all = total <= top;                                // everything is granted: what is left is known without the others
+  if (all && blockIdx.x == 0 && threadIdx.x == 0) a.n_free[0] = (int32_t)(top - total);
   if (b >= a.B) return;
   for (int i = b0; i < b; ++i) before += missing(i);
-  const int need = a.need[b], at = plan_grant(need, before, top);
+  const int at = plan_grant(need, before, top);
   if (lane == 0 && a.granted) a.granted[b] = at >= 0 ? 1 : 0;
   if (at < 0 || need == 0) return;
-  if (lane == 0) atomicMin(a.n_free, (int32_t)(top - before - need));
-  plan_take(a, b, lane, top - 1 - at);
+  if (!all && lane == 0) atomicMin(a.n_free, (int32_t)(top - before - need));   // (one address: 500 of them take 3 us)
+  plan_take(a, r, b, lane, top - 1 - at, e);
 }
 
 hipError_t launch_plan_pages(dllm_ctx* c, hipStream_t s, int n_pages, int B, int keep_head, const int32_t* length, const int32_t* first,
@@ -299,7 +315,7 @@ __global__ __launch_bounds__(1024) void k_slot_scan(const SlotArgs a) {
 // writes cu), so that the call is one launch.
 constexpr int SLOT_ONE = 4096, SLOT_WG = 2048;
 __global__ __launch_bounds__(256) void k_slot_map(const SlotArgs a, int own_scan, int wide) {
-  __shared__ int32_t s_cu[SLOT_ONE + 1], sm[4];
+  __shared__ int32_t s_cu[SLOT_ONE + 1], s_lo[SLOT_ONE], sm[4];
   const int tid = threadIdx.x;
   if (own_scan) {
     const int per = (a.B + 255) / 256;
@@ -309,7 +325,7 @@ __global__ __launch_bounds__(256) void k_slot_map(const SlotArgs a, int own_scan
       const int b = tid * per + i;
       int lo, hi;
       bool x;
-      if (b < a.B) { slot_range(a, b, lo, hi, x); bad |= x; sum += hi - lo; s_cu[b] = hi - lo; }
+      if (b < a.B) { slot_range(a, b, lo, hi, x); bad |= x; sum += hi - lo; s_cu[b] = hi - lo; s_lo[b] = lo; }
     }
     int32_t at = block_scan<256>(sum, tid, sm, total);
     for (int i = 0; i < per; ++i) {
@@ -330,6 +346,7 @@ __global__ __launch_bounds__(256) void k_slot_map(const SlotArgs a, int own_scan
   }
   const int32_t* const cu = own_scan ? s_cu : a.cu;
   const int n = cu[a.B];
+  auto start_of = [&](int b) { return own_scan ? s_lo[b] : (int)min((int64_t)max(a.start[b], 0), (int64_t)a.max_pages * a.pt); };
   for (int pass = 0; pass < SLOT_WG / 1024; ++pass) {
     const int64_t i0 = (int64_t)blockIdx.x * SLOT_WG + pass * 1024 + tid * 4;
     if (i0 >= a.capacity) return;
@@ -340,8 +357,7 @@ __global__ __launch_bounds__(256) void k_slot_map(const SlotArgs a, int own_scan
         const int mid = (b + end) >> 1;
         if (cu[mid] <= i0) b = mid; else end = mid;
       }
-      int first = cu[b], lo = a.start[b], page = -1, pi = -1;
-      lo = (int)min((int64_t)max(lo, 0), (int64_t)a.max_pages * a.pt);
+      int first = cu[b], lo = start_of(b), page = -1, pi = -1;
       int32_t o[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -351,7 +367,7 @@ __global__ __launch_bounds__(256) void k_slot_map(const SlotArgs a, int own_scan
           while (cu[b + 1] <= i) {
             ++b;
             first = cu[b];
-            lo = (int)min((int64_t)max(a.start[b], 0), (int64_t)a.max_pages * a.pt);
+            lo = start_of(b);
             pi = -1;
           }
           const int pos = lo + (int)(i - first), p = pos / a.pt;
