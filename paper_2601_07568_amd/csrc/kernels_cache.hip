@@ -149,8 +149,8 @@ __device__ inline void plan_take(const PlanArgs& a, const PlanRow& r, int b, int
 }
 
 // Small batches, one launch: a workgroup with a wave a sequence counts, sums, pushes and pops, a barrier between (what the waves write
-// for each other goes through the L1 that they share).  us in a graph, this / three launches: 8 rows of 40 entries 3.7 / 7.0, 16 of 64
-// 5.9 / 8.8, 16 of 512 7.6 / 9.2; two rows a wave: 32 of 64 10.2 / 9.3, 32 of 512 16.8 / 10.9.
+// for each other goes through the L1 that they share).  us in a graph, this / three launches: 8 rows of 40 entries 3.7 / 7.6, 16 of 64
+// 5.7 / 8.6, 16 of 512 7.3 / 9.9; two rows a wave: 32 of 64 10.2 / 9.3, 32 of 512 16.8 / 10.9.
 constexpr int PLAN_ONE_MAX = 16;
 static bool plan_one(int B, int max_pages) { return B <= PLAN_ONE_MAX && max_pages <= PLAN_ROW; }
 __global__ __launch_bounds__(1024) void k_plan_one(const PlanArgs a) {
